@@ -404,6 +404,133 @@ SC_API sc_status sc_append_layers(const sc_append_layer* layers /*DEVICE [L]*/, 
                            int32_t max_chunk_len, float tau, int32_t cap, int32_t* status, void* stream);
 
 /*
+ * A cache in pages.  A server that holds many sequences keeps their keys and values in pages of page_size rows
+ * out of one pool, and a table per sequence that says which pages are its own, so that a sequence takes memory
+ * as it grows.  Three calls work on such a cache: sc_paged_append writes rows, sc_paged_decode_attn attends to
+ * them, sc_paged_select picks the pages worth attending to.  The rows may be raw tokens or semantic cores with
+ * their counts.  (The paper keeps its caches contiguous; pages are this library's.)
+ *
+ *   k, v         pools, dtype dt: element (page p, head h, row r, column c) lies at p * page_stride + h * head_stride +
+ *                r * row_stride + c, so a page may be head-major [heads, page_size, d] or token-major [page_size, heads, d].
+ *                Strides are in elements, 16-byte multiples; row_stride >= d; 16-byte aligned.
+ *   num_pages    pages in the pool;  page_size >= 1 rows, any number
+ *   page_heads   KV heads that a page holds rows of: Hkv, or 1 where every head has pages of its own (h is 0 then)
+ *   table        int32: entry j of table (b, ht) lies at (b * table_heads + ht) * table_stride + j and names the page that
+ *                holds rows [j * page_size, (j + 1) * page_size).  Entries behind a table's last row are not looked at.
+ *   table_heads  tables per sequence: 1 (all its KV heads share one), or Hkv (a compressed cache, whose heads differ in
+ *                length, or the choice sc_paged_select made).  page_heads == 1 needs table_heads == Hkv.
+ *   max_pages    entries per table; max_pages * page_size <= 2^31 - 1
+ *   count        int32 [num_pages, page_heads, page_size], or NULL: every row has count 1
+ *   k_min, k_max dtype dt [num_pages, page_heads, d], or NULL: smallest and largest key of each page and column
+ *
+ * A table entry that a call needs and that names no page (negative, or >= num_pages) sets the status word to
+ * SC_ERR_INVALID_ARG; nothing is read or written through it.
+ */
+typedef struct {
+    void* k; void* v;
+    int64_t page_stride, head_stride, row_stride;
+    int32_t num_pages, page_size, page_heads;
+    const int32_t* table; int64_t table_stride; int32_t table_heads, max_pages;
+    int32_t* count;
+    void* k_min; void* k_max;
+} sc_paged_cache;
+
+#define SC_FLAG_ROPE_PAIRS 32u  /* sc_paged_append only: neighbouring columns (2i, 2i+1) are rotated together instead of
+                                  columns i and i + rot_dim / 2 */
+
+/*
+ * Rows join a paged cache, the position rotation applied on the way.  Row i of sequence b (token seq_off[b] + i of the
+ * arrays below) becomes row cache_len[b] + i of the sequence's cache.  One call takes a ragged batch: chunks of
+ * prompts, single generated tokens, or both.
+ *
+ * The rotation (inv_freq not NULL) turns each pair (x1, x2) of the first rot_dim columns of a key or query by the angle
+ * a_i = position * inv_freq[i]:  y1 = x1 cos a_i - x2 sin a_i,  y2 = x2 cos a_i + x1 sin a_i.  The angle is taken in 64
+ * bits, so far positions lose nothing; products in fp32, one rounding to dt.  Values and the columns behind rot_dim
+ * are copied.
+ *
+ *   rows (HOST)
+ *     k, v        [T, Hkv, d], dtype dt, element strides kv_token, kv_head (16-byte multiples; d contiguous)
+ *     count       [T, Hkv] int32, or NULL: written as 1 where the cache has counts (and refused where it has none)
+ *     seq_off     [B + 1] int32 (device), not falling, 0 <= seq_off[b] <= T: sequence b's tokens start at seq_off[b]
+ *     seq_len     [B] int32 (device) with 0 <= seq_len[b] <= seq_off[b+1] - seq_off[b], or NULL: all of that range.
+ *                 Tokens outside every sequence's range are not looked at.
+ *     cache_len   [B] int32 (device): rows each sequence holds already
+ *     len_out     [B] int32 (device), may be NULL: cache_len[b] + its new rows.  Not cache_len itself: all layers of
+ *                 a model append at the same place, so the lengths move on once per step, not once per call.
+ *     q, q_out    [T, Hq, d] queries of the same tokens and where they go rotated; both NULL to skip.  Element strides
+ *                 q_token, q_head and qo_token, qo_head (16-byte multiples); q_out may be q itself.
+ *     inv_freq    [rot_dim / 2] float (device), or NULL: no rotation;  rot_dim even, 0..d
+ *     positions   [T] int32 (device), or NULL: a token's position is the row it gets
+ *   cache       its tables are [B, 1, max_pages] and its pages hold all Hkv heads.  A cache with tables and pages per head is
+ *               appended to as B * Hkv sequences of one head each; so does the output of sc_compress get into pages: T =
+ *               B * Hkv * cap, seq_off[i] = i * cap, seq_len = core_len, count, no rotation.
+ *               Where k_min and k_max are given they are brought up to date: a page whose first row is new starts afresh,
+ *               another one's bounds are widened.  (NaN keys make the bound of their column NaN.)
+ *   flags       SC_FLAG_ROPE_PAIRS or 0
+ *   status      SC_ERR_CAPACITY if a sequence's new rows do not all fit its table: its cache stays as it is and its
+ *               len_out is cache_len (queries are rotated all the same).  SC_ERR_INVALID_ARG for offsets or lengths that
+ *               break the rules above: that sequence is passed over.
+ * No two sequences may append to the same page.  One kernel launch; no workspace.
+ */
+typedef struct {
+    const void* k; const void* v; int64_t kv_token, kv_head;
+    const int32_t* count;
+    const int32_t* seq_off; const int32_t* seq_len; const int32_t* cache_len; int32_t* len_out;
+    const void* q; void* q_out; int64_t q_token, q_head, qo_token, qo_head;
+    const float* inv_freq; int32_t rot_dim; const int32_t* positions;
+} sc_paged_rows;
+
+SC_API sc_status sc_paged_append(const sc_paged_cache* cache /*HOST*/, const sc_paged_rows* rows /*HOST*/, sc_dtype dt, int32_t B,
+                          int32_t Hq, int32_t Hkv, int32_t T, int32_t d, uint32_t flags, int32_t* status, void* stream);
+
+/*
+ * One decode step of Proportional Attention over a paged cache: sc_decode_attn with the rows found through the tables.
+ *     x_t = scale * <q, k_t> + ln(count_t),  out = sum_t softmax(x)_t * v_t   over the rows t < lens[b, ht]
+ * The rows of all sequences are shared out evenly among the launch's blocks whatever the lengths are; a head that
+ * several blocks (or clusters of blocks) share is joined at the end in a fixed order.
+ *
+ *   q, out     [B, Hq, d] contiguous, dtype dt
+ *   lens       [B, table_heads] int32 (device); more than max_pages * page_size counts as that many, below 0 as none
+ *   scale      0 means 1/sqrt(d)
+ *   flags      SC_FLAG_GENERIC forces the generic kernels; else 0
+ *   workspace  at least sc_paged_decode_workspace_bytes(B, Hq, Hkv, d) bytes, 16-byte aligned, whatever the lengths.  Its
+ *              arrival counters must be zero on entry and are left zero: zero the workspace once after allocating it.
+ *              Calls that share a workspace must not overlap.
+ *   status     SC_ERR_INVALID_ARG: a table named no page (its rows are left out of the sums); SC_ERR_TIMEOUT: a bounded
+ *              wait inside the kernel gave up, the outputs it was for are not a number
+ * A head without rows gets zeros.
+ */
+SC_API size_t sc_paged_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
+
+SC_API sc_status sc_paged_decode_attn(const sc_paged_cache* cache /*HOST*/, const void* q, sc_dtype dt, int32_t B, int32_t Hq,
+                               int32_t Hkv, int32_t d, const int32_t* lens, float scale, uint32_t flags, void* out,
+                               void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * Sparse attention's choice of pages: for every (sequence b, KV head h) the `keep` pages whose keys can score highest, by
+ *     bound_p = max over the head's queries g of  sum_c max(q_gc * k_min[p, h, c], q_gc * k_max[p, h, c])
+ * which no <q_g, k_t> of the page's rows exceeds.  The first n_first and the last n_last pages of a sequence are always
+ * among them.  Equal bounds: the earlier page.  A bound that is not a number ranks above all numbers.  The choice is the one that
+ * bounds in 64 bits give.
+ * The result is a table for sc_paged_decode_attn (the same cache with table = sel_table, table_heads = Hkv, max_pages =
+ * table_stride = keep, and lens = sel_len): attention over the pages picked costs what keep pages cost, however long the cache.
+ *
+ *   cache       with k_min and k_max (k, v and count are not looked at)
+ *   q           [B, Hq, d] contiguous, dtype dt;  lens [B, table_heads] as for sc_paged_decode_attn
+ *   keep        >= 1;  n_first >= 0, n_last >= 1, n_first + n_last <= keep
+ *   sel_table   out [B, Hkv, keep] int32: the picked pages' table entries in the order of their rows; -1 behind them where a
+ *               sequence has fewer pages (all of them are picked then)
+ *   sel_len     out [B, Hkv] int32: rows in the picked pages
+ *   status      SC_ERR_INVALID_ARG: a table named no page; its bound ranks below all others
+ * max_pages at most SC_SELECT_MAX_PAGES (else SC_ERR_UNSUPPORTED).  One kernel launch; no workspace.
+ */
+#define SC_SELECT_MAX_PAGES 262144
+
+SC_API sc_status sc_paged_select(const sc_paged_cache* cache /*HOST*/, const void* q, sc_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
+                          int32_t d, const int32_t* lens, int32_t keep, int32_t n_first, int32_t n_last, int32_t* sel_table,
+                          int32_t* sel_len, int32_t* status, void* stream);
+
+/*
  * sc_decode_attn for callers that cannot allocate device memory.  (A convenience of this
  * library; the paper has no counterpart.)
  *

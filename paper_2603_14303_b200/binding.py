@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libsemanticache.so")
 SC_OK, SC_ERR_INVALID_ARG, SC_ERR_UNSUPPORTED, SC_ERR_CAPACITY, SC_ERR_CUDA, SC_ERR_TIMEOUT = range(6)
 SC_BF16, SC_F32 = 0, 1
 SC_FLAG_GENERIC, SC_FLAG_TWO_PASS, SC_FLAG_OVERLAP_PREV, SC_FLAG_OVERLAP_CHAIN, SC_FLAG_CAUSAL_TAIL = 1, 2, 4, 8, 16
+SC_FLAG_ROPE_PAIRS = 32
+SC_SELECT_MAX_PAGES = 262144
 SC_MAX_CHUNK_LEN, SC_MAX_DELIMS, SC_TILE_ROWS = 256, 64, 128
 _STATUS_NAMES = ["SC_OK", "SC_ERR_INVALID_ARG", "SC_ERR_UNSUPPORTED", "SC_ERR_CAPACITY", "SC_ERR_CUDA",
                  "SC_ERR_TIMEOUT"]
@@ -28,7 +30,8 @@ EXPORTS = ["sc_version", "sc_launch_counter", "sc_chunk_bounds", "sc_chunk_works
            "sc_compress_workspace_bytes", "sc_compress", "sc_decode_workspace_bytes", "sc_decode_attn",
            "sc_decode_attn_static", "sc_append", "sc_compress_budget_workspace_bytes", "sc_compress_budget",
            "sc_compress_global_workspace_bytes", "sc_compress_global", "sc_prefill_attn", "sc_append_layers",
-           "sc_compress_layers_workspace_bytes", "sc_compress_layers"]
+           "sc_compress_layers_workspace_bytes", "sc_compress_layers", "sc_paged_append", "sc_paged_decode_workspace_bytes",
+           "sc_paged_decode_attn", "sc_paged_select"]
 SC_MAX_LAYERS_PER_CALL = 64
 SC_BUDGET_MAX_GRID = 65
 SC_STATIC_SCRATCH_BYTES = 8 << 20
@@ -55,6 +58,22 @@ class _CompressLayer(ctypes.Structure):
 
 class _Strides(ctypes.Structure):
     _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("page_heads", ctypes.c_int32), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("table_heads", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("count", ctypes.c_void_p),
+                ("k_min", ctypes.c_void_p), ("k_max", ctypes.c_void_p)]
+
+
+class _PagedRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kv_token", ctypes.c_int64), ("kv_head", ctypes.c_int64),
+                ("count", ctypes.c_void_p), ("seq_off", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("cache_len", ctypes.c_void_p),
+                ("len_out", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("q_token", ctypes.c_int64),
+                ("q_head", ctypes.c_int64), ("qo_token", ctypes.c_int64), ("qo_head", ctypes.c_int64), ("inv_freq", ctypes.c_void_p),
+                ("rot_dim", ctypes.c_int32), ("positions", ctypes.c_void_p)]
 
 
 _lib = None
@@ -115,6 +134,16 @@ def lib() -> ctypes.CDLL:
         L.sc_append.restype = _i32
         L.sc_append.argtypes = [_vp, _vp, _i32, _i32, _i32, _i32, _vp, ctypes.POINTER(_i32), _i32, _i32, ctypes.c_float,
                                 _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]
+        cache = ctypes.POINTER(_PagedCache)
+        L.sc_paged_append.restype = _i32
+        L.sc_paged_append.argtypes = [cache, ctypes.POINTER(_PagedRows), _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_uint32, _vp, _vp]
+        L.sc_paged_decode_workspace_bytes.restype = _sz
+        L.sc_paged_decode_workspace_bytes.argtypes = [_i32] * 4
+        L.sc_paged_decode_attn.restype = _i32
+        L.sc_paged_decode_attn.argtypes = [cache, _vp, _i32, _i32, _i32, _i32, _i32, _vp, ctypes.c_float, ctypes.c_uint32, _vp, _vp, _sz,
+                                           _vp, _vp]
+        L.sc_paged_select.restype = _i32
+        L.sc_paged_select.argtypes = [cache, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
         _lib = L
     return _lib
 
@@ -514,3 +543,221 @@ def decode_attn(q, layer: CompressedLayer, out=None, workspace=None, scale: floa
     sc_decode_attn(q, layer.core_k, layer.core_v, layer.count if use_count else None, layer.core_len, out,
                    workspace, scale, status, flags)
     return out
+
+
+# ------------------------------------------------------------------------------- a cache in pages
+
+
+def _step(t: torch.Tensor, dim: int) -> int:
+    """Stride of an axis; 0 where it has one entry (torch may say anything there)."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+@dataclasses.dataclass(frozen=True)
+class PagedCache:
+    """One layer's keys and values in pages (``sc_paged_cache`` of the header).
+
+    ``k``, ``v``: [pages, heads, page_size, d], any strides with d contiguous (token-major storage is the transposed view of
+    [pages, page_size, heads, d]); ``heads`` is Hkv, or 1 where every head has pages of its own.  ``table``: int32
+    [B, max_pages], or [B, Hkv, max_pages] with a table per head ([B, 1, max_pages] is the first form).  ``count``: int32
+    [pages, heads, page_size] for a cache of semantic cores.  ``k_min``, ``k_max``: [pages, heads, d], kept by paged_append
+    and read by paged_select."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    count: torch.Tensor | None = None
+    k_min: torch.Tensor | None = None
+    k_max: torch.Tensor | None = None
+
+    def __post_init__(self):
+        k, v, table = self.k, self.v, self.table
+        _need_cuda(k, v, table, self.count, self.k_min, self.k_max)
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or any(_step(k, i) != _step(v, i) for i in range(3)):
+            raise ValueError("k and v: [pages, heads, page_size, d] of one type and layout")
+        P, heads, ps, d = k.shape
+        if d > 1 and (k.stride(3) != 1 or v.stride(3) != 1):
+            raise ValueError("the head dimension of k and v must be contiguous")
+        if table.dim() not in (2, 3) or table.dtype != torch.int32:
+            raise ValueError("table: int32 [B, max_pages] or [B, heads, max_pages]")
+        th, W = (table.shape[1] if table.dim() == 3 else 1), table.shape[-1]
+        stride = table.stride(-2) if table.shape[-2] > 1 else table.stride(0) if table.shape[0] > 1 else W
+        if (W > 1 and table.stride(-1) != 1) or stride < W or (table.dim() == 3 and table.shape[0] > 1 and table.stride(0) != th * stride):
+            raise ValueError("table: rows evenly spaced, entries contiguous")
+        if self.count is not None and (self.count.dtype != torch.int32 or self.count.shape != (P, heads, ps) or not self.count.is_contiguous()):
+            raise ValueError("count: contiguous int32 [pages, heads, page_size]")
+        if (self.k_min is None) != (self.k_max is None):
+            raise ValueError("k_min and k_max go together")
+        for t in (self.k_min, self.k_max):
+            if t is not None and (t.dtype != k.dtype or t.shape != (P, heads, d) or not t.is_contiguous()):
+                raise ValueError("k_min, k_max: contiguous [pages, heads, d] of the cache's type")
+        dev = k.get_device()
+        if any(t is not None and t.get_device() != dev for t in (v, table, self.count, self.k_min, self.k_max)):
+            raise ValueError("the parts of a cache live on one device")
+        form = _PagedCache(None, None, _step(k, 0), _step(k, 1), k.stride(2) if ps > 1 else d, P, ps, heads, None, stride, th, W, None, None,
+                           None)
+        for name, value in (("B", table.shape[0]), ("heads", heads), ("table_heads", th), ("d", d), ("_dt", _dt(k)), ("_dev", dev),
+                            ("_form", bytes(form))):
+            object.__setattr__(self, name, value)
+
+    def over(self, table: torch.Tensor) -> "PagedCache":
+        """The same pages through another table: paged_select's choice, another batch."""
+        return dataclasses.replace(self, table=table)
+
+    def one_head_sequences(self) -> "PagedCache":
+        """A cache with tables and pages per head as B * Hkv sequences of one head each, the form in which it is appended to."""
+        if self.heads != 1 or self.table.dim() != 3:
+            raise ValueError("tables and pages per head required")
+        return self.over(self.table.reshape(self.B * self.table_heads, 1, self.table.shape[2]))
+
+    def _pointers(self):
+        return (self.k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(), _ptr(self.count), _ptr(self.k_min), _ptr(self.k_max),
+                self._form)
+
+
+def _same_device(cache: PagedCache, *ts):
+    for t in ts:
+        if t is not None and t.get_device() != cache._dev:
+            raise ValueError("tensors of the cache's device required")
+
+
+def _lengths(t: torch.Tensor, n: int, what: str):
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous int32")
+
+
+def _called(name: str, dev: int, *args):
+    """A call of the native extension with ``dev`` as the current device."""
+    fn = getattr(_native(), name)
+    if dev == torch.cuda.current_device():
+        code = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            code = fn(*args)
+    if code != SC_OK:
+        raise ScError("sc_" + name, code)
+
+
+def sc_paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, seq_len=None, count_new=None, len_out=None, q=None, q_out=None,
+                    inv_freq=None, positions=None, status=None, flags=0):
+    """Raw sc_paged_append: rows k_new, v_new [T, Hkv, d] join the cache of their sequences (see the header).  ``inv_freq``
+    (float32) turns the first 2 * len(inv_freq) columns of the keys, and of ``q`` [T, Hq, d] on its way to ``q_out``."""
+    _same_device(cache, k_new, v_new, seq_off, cache_len, seq_len, count_new, len_out, q, q_out, inv_freq, positions, status)
+    T, Hkv, d = k_new.shape
+    B = cache.B
+    if v_new.shape != k_new.shape or Hkv != cache.heads or d != cache.d:
+        raise ValueError("k_new and v_new: [T, heads, d] as the cache's pages")
+    ks = (_step(k_new, 0), _step(k_new, 1))
+    if k_new.stride(2) != 1 or v_new.stride(2) != 1 or ks != (_step(v_new, 0), _step(v_new, 1)):
+        raise ValueError("k_new and v_new: one layout, d contiguous")
+    if k_new.dtype != cache.k.dtype or v_new.dtype != cache.k.dtype:
+        raise TypeError("k_new and v_new must have the cache's type")
+    _lengths(seq_off, B + 1, "seq_off")
+    _lengths(cache_len, B, "cache_len")
+    for t, n, what in ((seq_len, B, "seq_len"), (len_out, B, "len_out"), (count_new, T * Hkv, "count_new"), (positions, T, "positions")):
+        if t is not None:
+            _lengths(t, n, what)
+    Hq, qs, qos = Hkv, (0, 0), (0, 0)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        Hq = q.shape[1]
+        if q.shape != (T, Hq, d) or q_out.shape != q.shape or q.stride(2) != 1 or q_out.stride(2) != 1:
+            raise ValueError("q and q_out: [T, Hq, d], d contiguous")
+        if q.dtype != cache.k.dtype or q_out.dtype != cache.k.dtype:
+            raise TypeError("q and q_out must have the cache's type")
+        qs, qos = (_step(q, 0), _step(q, 1)), (_step(q_out, 0), _step(q_out, 1))
+    rot = 0
+    if inv_freq is not None:
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq: contiguous float32")
+        rot = 2 * inv_freq.numel()
+    _called("paged_append", cache._dev, *cache._pointers(), k_new.data_ptr(), v_new.data_ptr(), *ks, _ptr(count_new), seq_off.data_ptr(),
+            _ptr(seq_len), cache_len.data_ptr(), _ptr(len_out), _ptr(q), _ptr(q_out), *qs, *qos, _ptr(inv_freq), rot, _ptr(positions),
+            cache._dt, B, Hq, Hkv, T, d, int(flags), _ptr(status), _stream(k_new))
+
+
+def sc_paged_decode_attn(q, cache: PagedCache, lens, out, workspace, scale=0.0, status=None, flags=0):
+    """Raw sc_paged_decode_attn: one decode step over a paged cache, q/out [B, Hq, d], lens int32 [B] or [B, table_heads]."""
+    _same_device(cache, q, lens, out, workspace, status)
+    B, Hq, d = q.shape
+    th = cache.table_heads
+    Hkv = cache.heads if cache.heads > 1 else th
+    if B != cache.B or d != cache.d or out.shape != q.shape or not q.is_contiguous() or not out.is_contiguous():
+        raise ValueError("q and out: contiguous [B, Hq, d] as the cache")
+    if q.dtype != cache.k.dtype or out.dtype != q.dtype:
+        raise TypeError("q and out must have the cache's type")
+    _lengths(lens, B * th, "lens")
+    _called("paged_decode_attn", cache._dev, *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, d, lens.data_ptr(), float(scale), int(flags),
+            out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(q))
+
+
+def sc_paged_select(q, cache: PagedCache, lens, keep, n_first, n_last, sel_table, sel_len, status=None):
+    """Raw sc_paged_select: the ``keep`` pages of every (sequence, KV head) whose keys can score highest (see the header)."""
+    _same_device(cache, q, lens, sel_table, sel_len, status)
+    B, Hq, d = q.shape
+    th = cache.table_heads
+    Hkv = cache.heads if cache.heads > 1 else th
+    if B != cache.B or d != cache.d or not q.is_contiguous():
+        raise ValueError("q: contiguous [B, Hq, d] as the cache")
+    if q.dtype != cache.k.dtype:
+        raise TypeError("q must have the cache's type")
+    if cache.k_min is None:
+        raise ValueError("a cache with k_min and k_max required")
+    _lengths(lens, B * th, "lens")
+    _lengths(sel_table, B * Hkv * keep, "sel_table")
+    _lengths(sel_len, B * Hkv, "sel_len")
+    _called("paged_select", cache._dev, *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, d, lens.data_ptr(), int(keep), int(n_first),
+            int(n_last), sel_table.data_ptr(), sel_len.data_ptr(), _ptr(status), _stream(q))
+
+
+def paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, *, seq_len=None, count_new=None, inv_freq=None, positions=None,
+                 interleaved: bool = False, q=None, q_out=None, len_out=None, status=None):
+    """New rows join a paged cache, keys (and queries) rotated on the way.  Returns (the sequences' new lengths, the rotated
+    queries or None).  All layers of a model append at the same ``cache_len``: move it on once per step."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if len_out is None:
+        len_out = torch.empty_like(cache_len)
+    sc_paged_append(cache, k_new, v_new, seq_off, cache_len, seq_len, count_new, len_out, q, q_out, inv_freq, positions, status,
+                    SC_FLAG_ROPE_PAIRS if interleaved else 0)
+    return len_out, q_out
+
+
+def paged_store(layer: CompressedLayer, cache: PagedCache, cache_len=None, status=None):
+    """Puts a layer's semantic cores, counts with them, into pages: ``cache`` has tables and pages per head.  ``cache_len`` int32
+    [B, Hkv]: rows the heads hold already (none by default).  Returns the heads' new lengths [B, Hkv]."""
+    B, Hkv, cap, d = layer.core_k.shape
+    dev = layer.core_k.device
+    if cache_len is None:
+        cache_len = torch.zeros((B, Hkv), dtype=torch.int32, device=dev)
+    off = torch.arange(B * Hkv + 1, dtype=torch.int32, device=dev) * cap
+    # (a compression that found too little room says how much it needed; the rows behind cap were never written)
+    lens, _ = paged_append(cache.one_head_sequences(), layer.core_k.view(-1, 1, d), layer.core_v.view(-1, 1, d), off, cache_len,
+                           seq_len=layer.core_len.clamp(max=cap), count_new=layer.count.view(-1), status=status)
+    return lens
+
+
+def paged_decode_workspace(B, Hq, Hkv, d, device) -> torch.Tensor:
+    """Zero-initialised workspace for sc_paged_decode_attn (its arrival counters must start at zero)."""
+    return torch.zeros(lib().sc_paged_decode_workspace_bytes(B, Hq, Hkv, d), dtype=torch.uint8, device=device)
+
+
+def paged_decode_attn(q, cache: PagedCache, lens, out=None, workspace=None, scale: float = 0.0, status=None, flags: int = 0):
+    """One decode step of Proportional Attention over a paged cache (plain attention where it has no counts)."""
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        B, Hq, d = q.shape
+        workspace = paged_decode_workspace(B, Hq, cache.heads if cache.heads > 1 else cache.table_heads, d, q.device)
+    sc_paged_decode_attn(q, cache, lens, out, workspace, scale, status, flags)
+    return out
+
+
+def paged_select(q, cache: PagedCache, lens, keep: int, n_first: int = 0, n_last: int = 1, status=None):
+    """Picks pages for sparse attention.  Returns (table [B, Hkv, keep], lengths [B, Hkv]) for
+    ``paged_decode_attn(q, cache.over(table), lengths)``."""
+    Hkv = cache.heads if cache.heads > 1 else cache.table_heads
+    table = torch.empty((cache.B, Hkv, keep), dtype=torch.int32, device=q.device)
+    lengths = torch.empty((cache.B, Hkv), dtype=torch.int32, device=q.device)
+    sc_paged_select(q, cache, lens, keep, n_first, n_last, table, lengths, status)
+    return table, lengths

@@ -3,6 +3,7 @@
  * about 4 us to marshal such a call (eighteen arguments), this 0.5 us; the GIL is released meanwhile, as ctypes does. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <string.h>
 
 #include "semanticache.h"
 
@@ -133,8 +134,58 @@ static PyObject* append_layers(PyObject* self, PyObject* const* a, Py_ssize_t n)
     CALL(sc_append_layers(table, L, dt, B, H, d, ids, delims, nd, max_len, tau, cap, status, stream));
 }
 
+/* a cache in pages: its six addresses, and the bytes of an sc_paged_cache that has everything but them */
+static int cache_of(PyObject* const* a, sc_paged_cache* c) {
+    char* form;
+    Py_ssize_t n;
+    if (PyBytes_AsStringAndSize(a[6], &form, &n) < 0) return 0;
+    if (n != (Py_ssize_t)sizeof *c) { PyErr_SetString(PyExc_ValueError, "not the form of a paged cache"); return 0; }
+    memcpy(c, form, sizeof *c);
+    c->k = ptr(a[0]); c->v = ptr(a[1]); c->table = ptr(a[2]); c->count = ptr(a[3]); c->k_min = ptr(a[4]); c->k_max = ptr(a[5]);
+    return 1;
+}
+static int64_t i64(PyObject* o) { return PyLong_AsLongLong(o); }
+static PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    sc_paged_cache c;
+    sc_paged_rows r;
+    (void)self;
+    if (!arity(n, 34, "paged_append") || !cache_of(a, &c)) return NULL;
+    r.k = ptr(a[7]); r.v = ptr(a[8]); r.kv_token = i64(a[9]); r.kv_head = i64(a[10]); r.count = ptr(a[11]); r.seq_off = ptr(a[12]);
+    r.seq_len = ptr(a[13]); r.cache_len = ptr(a[14]); r.len_out = ptr(a[15]); r.q = ptr(a[16]); r.q_out = ptr(a[17]);
+    r.q_token = i64(a[18]); r.q_head = i64(a[19]); r.qo_token = i64(a[20]); r.qo_head = i64(a[21]); r.inv_freq = ptr(a[22]);
+    r.rot_dim = i32(a[23]); r.positions = ptr(a[24]);
+    const sc_dtype dt = (sc_dtype)i32(a[25]);
+    const int32_t B = i32(a[26]), Hq = i32(a[27]), Hkv = i32(a[28]), T = i32(a[29]), d = i32(a[30]);
+    const uint32_t flags = u32(a[31]);
+    void *status = ptr(a[32]), *stream = ptr(a[33]);
+    CALL(sc_paged_append(&c, &r, dt, B, Hq, Hkv, T, d, flags, status, stream));
+}
+static PyObject* paged_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    sc_paged_cache c;
+    (void)self;
+    if (!arity(n, 21, "paged_decode_attn") || !cache_of(a, &c)) return NULL;
+    const void *q = ptr(a[7]), *lens = ptr(a[13]);
+    const sc_dtype dt = (sc_dtype)i32(a[8]);
+    const int32_t B = i32(a[9]), Hq = i32(a[10]), Hkv = i32(a[11]), d = i32(a[12]);
+    const float scale = f32(a[14]);
+    const uint32_t flags = u32(a[15]);
+    void *out = ptr(a[16]), *ws = ptr(a[17]), *status = ptr(a[19]), *stream = ptr(a[20]);
+    const size_t bytes = sz(a[18]);
+    CALL(sc_paged_decode_attn(&c, q, dt, B, Hq, Hkv, d, lens, scale, flags, out, ws, bytes, status, stream));
+}
+static PyObject* paged_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    sc_paged_cache c;
+    (void)self;
+    if (!arity(n, 21, "paged_select") || !cache_of(a, &c)) return NULL;
+    const void *q = ptr(a[7]), *lens = ptr(a[13]);
+    const sc_dtype dt = (sc_dtype)i32(a[8]);
+    const int32_t B = i32(a[9]), Hq = i32(a[10]), Hkv = i32(a[11]), d = i32(a[12]), keep = i32(a[14]), first = i32(a[15]), last = i32(a[16]);
+    void *table = ptr(a[17]), *len = ptr(a[18]), *status = ptr(a[19]), *stream = ptr(a[20]);
+    CALL(sc_paged_select(&c, q, dt, B, Hq, Hkv, d, lens, keep, first, last, table, len, status, stream));
+}
+
 #define FN(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FN(chunk_sizes), FN(chunk), FN(compress), FN(decode_attn), FN(prefill_attn), FN(append), FN(append_layers),
-                                {NULL, NULL, 0, NULL}};
+                                FN(paged_append), FN(paged_decode_attn), FN(paged_select), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__native_calls(void) { return PyModule_Create(&module); }
