@@ -498,7 +498,8 @@ SC_API sc_status sc_paged_append(const sc_paged_cache* cache /*HOST*/, const sc_
  *              Calls that share a workspace must not overlap.
  *   status     SC_ERR_INVALID_ARG: a table named no page (its rows are left out of the sums); SC_ERR_TIMEOUT: a bounded
  *              wait inside the kernel gave up, the outputs it was for are not a number
- * A head without rows gets zeros.
+ * A head without rows gets zeros.  B * Hkv * ceil(Hq / Hkv / 4) * ceil(max_pages * page_size / 16) must stay below 2^31 (else
+ * SC_ERR_UNSUPPORTED).
  */
 SC_API size_t sc_paged_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
 
@@ -524,7 +525,7 @@ SC_API sc_status sc_paged_decode_attn(const sc_paged_cache* cache /*HOST*/, cons
  *   status      SC_ERR_INVALID_ARG: a table named no page; its bound ranks below all others
  * max_pages at most SC_SELECT_MAX_PAGES (else SC_ERR_UNSUPPORTED).  One kernel launch; no workspace.
  */
-#define SC_SELECT_MAX_PAGES 262144
+#define SC_SELECT_MAX_PAGES 131072
 
 SC_API sc_status sc_paged_select(const sc_paged_cache* cache /*HOST*/, const void* q, sc_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
                           int32_t d, const int32_t* lens, int32_t keep, int32_t n_first, int32_t n_last, int32_t* sel_table,

@@ -21,7 +21,7 @@ SC_OK, SC_ERR_INVALID_ARG, SC_ERR_UNSUPPORTED, SC_ERR_CAPACITY, SC_ERR_CUDA, SC_
 SC_BF16, SC_F32 = 0, 1
 SC_FLAG_GENERIC, SC_FLAG_TWO_PASS, SC_FLAG_OVERLAP_PREV, SC_FLAG_OVERLAP_CHAIN, SC_FLAG_CAUSAL_TAIL = 1, 2, 4, 8, 16
 SC_FLAG_ROPE_PAIRS = 32
-SC_SELECT_MAX_PAGES = 262144
+SC_SELECT_MAX_PAGES = 131072
 SC_MAX_CHUNK_LEN, SC_MAX_DELIMS, SC_TILE_ROWS = 256, 64, 128
 _STATUS_NAMES = ["SC_OK", "SC_ERR_INVALID_ARG", "SC_ERR_UNSUPPORTED", "SC_ERR_CAPACITY", "SC_ERR_CUDA",
                  "SC_ERR_TIMEOUT"]

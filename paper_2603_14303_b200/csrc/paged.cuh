@@ -43,51 +43,71 @@ struct Line {
     int entries, per_entry, cap, tile, parties;   // per_entry: units of an entry
 
     __device__ __forceinline__ int len(int e) const { return max(min(lens[e], cap), 0); }
-    __device__ __forceinline__ int tiles(int e) const { return (len(e) + tile - 1) / tile; }
+    __host__ __device__ __forceinline__ int tiles_of(int n) const { return n > 0 ? (int)((unsigned)(n - 1) / (unsigned)tile) + 1 : 0; }   // (n may be 2^31 - 1)
+    __device__ __forceinline__ int tiles(int e) const { return tiles_of(len(e)); }
+    // Positions on the line are 32-bit numbers, which the entry point sees to: several divisions lie on the way to the first load.
 };
 struct Place {              // a position on the line
     int entry, unit, tile;
-    int64_t at;             // of the unit's first tile
+    unsigned at;            // of the unit's first tile
 };
 
-// Length of a party's stretch.  All lanes of a warp call it; every warp of the launch gets the same.
-__device__ __forceinline__ int64_t stretch_of(const Line& line, int least, int lane, int64_t& total) {
-    int64_t sum = 0;
+// Length of the line.  All lanes of a warp call it.
+__device__ __forceinline__ unsigned total_of(const Line& line, int lane) {
+    unsigned sum = 0;
 #pragma unroll 4
     for (int e = lane; e < line.entries; e += 32) sum += line.tiles(e);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-    total = sum * line.per_entry;
-    const int64_t each = (total + line.parties - 1) / line.parties;
-    return each > least ? each : least;
+    return __reduce_add_sync(kFull, sum) * line.per_entry;
 }
 
 // The place of tile `at` of the line (at < total).  All lanes of a warp call it.
-__device__ __forceinline__ Place place_of(const Line& line, int64_t at, int lane) {
-    int64_t before = 0;
+__device__ __forceinline__ Place place_of(const Line& line, unsigned at, int lane) {
+    unsigned before = 0;
     for (int e0 = 0;; e0 += 32) {
         const int nt = e0 + lane < line.entries ? line.tiles(e0 + lane) : 0;
-        const int64_t mine = (int64_t)nt * line.per_entry;
-        int64_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t t = __shfl_up_sync(kFull, upto, o);
-            if (lane >= o) upto += t;
-        }
-        const unsigned past = __ballot_sync(kFull, before + upto > at);
+        const unsigned mine = (unsigned)nt * line.per_entry, upto = before + warp_scan_add((int)mine, lane);
+        const unsigned past = __ballot_sync(kFull, upto > at);
         if (past != 0) {
             const int src = __ffs(past) - 1;
-            const int64_t start = before + __shfl_sync(kFull, upto - mine, src);
-            const int t = __shfl_sync(kFull, nt, src);
+            const unsigned start = __shfl_sync(kFull, upto - mine, src), t = __shfl_sync(kFull, nt, src);
             Place p;
             p.entry = e0 + src;
-            p.unit = (int)((at - start) / t);
-            p.at = start + (int64_t)p.unit * t;
-            p.tile = (int)(at - p.at);
+            p.unit = (at - start) / t;
+            p.at = start + p.unit * t;
+            p.tile = at - p.at;
             return p;
         }
-        before += __shfl_sync(kFull, upto, 31);
+        before = __shfl_sync(kFull, upto, 31);
     }
+}
+
+// A line whose stretches would be short is cut at the units' ends instead, so that a party has one segment and fills its pipeline once:
+// every unit in as many equal parts as have `longest` tiles at most, `longest` the least for which there are parties enough (at most an
+// eighth over it).  For at most 64 entries and no more units than parties.  All lanes of a warp call it.
+struct Part { int entry, unit, tile, take, index, parts; };   // take 0: this party has none
+__device__ __forceinline__ Part part_of(const Line& line, unsigned longest, unsigned party, int lane) {
+    const unsigned t0 = lane < line.entries ? line.tiles(lane) : 0, t1 = lane + 32 < line.entries ? line.tiles(lane + 32) : 0;
+    unsigned c0, c1, sum;
+    for (;; longest += longest / 8 + 1) {
+        c0 = (t0 + longest - 1) / longest; c1 = (t1 + longest - 1) / longest;
+        sum = __reduce_add_sync(kFull, c0 + c1) * line.per_entry;
+        if (sum <= (unsigned)line.parties) break;
+    }
+    Part r = {0, 0, 0, 0, 0, 0};
+    if (party >= sum) return r;
+    const unsigned m0 = c0 * line.per_entry, u0 = warp_scan_add((int)m0, lane), all0 = __shfl_sync(kFull, u0, 31);
+    const unsigned m1 = c1 * line.per_entry, u1 = all0 + warp_scan_add((int)m1, lane);
+    const bool second = party >= all0;
+    const int src = __ffs(__ballot_sync(kFull, (second ? u1 : u0) > party)) - 1;
+    const unsigned start = __shfl_sync(kFull, second ? u1 - m1 : u0 - m0, src), parts = __shfl_sync(kFull, second ? c1 : c0, src);
+    const unsigned nt = __shfl_sync(kFull, second ? t1 : t0, src), each = (nt + parts - 1) / parts;
+    r.entry = src + (second ? 32 : 0);
+    r.unit = (party - start) / parts;
+    r.index = (party - start) - r.unit * parts;
+    r.parts = parts;
+    r.tile = r.index * each;
+    r.take = min(each, nt - r.tile);   // ((parts - 1) * each < nt)
+    return r;
 }
 
 // The next unit that has tiles (one follows: the caller has tiles left).

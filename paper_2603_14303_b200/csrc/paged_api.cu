@@ -83,6 +83,8 @@ sc_status sc_paged_decode_attn(const sc_paged_cache* cache, const void* q, sc_dt
     if (s == SC_OK) s = check_pool(cache, dt, d);
     if (s != SC_OK) return s;
     if (!(scale == scale) || scale < 0.f || (flags & ~SC_FLAG_GENERIC)) return SC_ERR_INVALID_ARG;
+    const int64_t heads = (int64_t)B * Hkv * div_up(Hq / Hkv, 4);
+    if (heads * (((int64_t)cache->max_pages * cache->page_size + 15) / 16) > 0x7fffffff) return SC_ERR_UNSUPPORTED;
     if (B == 0) return SC_OK;
     if (!q || !out || !lens || !workspace) return SC_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return SC_ERR_INVALID_ARG;

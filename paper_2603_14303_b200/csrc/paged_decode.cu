@@ -1,6 +1,602 @@
+// Tensor-core bf16 decode attention over a paged cache (Eq. 4; d = 64, 128 or 256; up to eight query heads at a time), sm_100a.
+//
+// The rows of all heads form one line of 16-row tiles (paged.cuh).  A party, a cluster of blocks (or one block), takes a stretch
+// of it; its blocks share each segment's tiles out evenly and their warps take them in turn, each through a private ring of
+// cp.async stages in shared memory (16-byte chunks, XOR-swizzled so that ldmatrix is conflict free).  Per tile:
+//     S^T[16 keys x 8 heads]   = K_tile . q^T                (mma.m16n8k16, keys on M, heads on N)
+//     x = S^T * scale*log2(e) + log2(count)
+//     P^T = 2^(x - m)          (online softmax in fp32; the running maximum is common to the warp and raised only when a score
+//                               overtakes it by a margin, so weights stay below 2^8)
+//     O^T[d x 8 heads] += V_tile^T . P^T                     (P as a bf16 pair, leading part + remainder: sixteen bits of each weight)
+// Up to four query heads stand in the eight columns twice, the second time for the remainders.  Warps meet in shared memory, blocks of a
+// cluster hand each other slices of their sums through distributed shared memory (decode_fold.cuh), parties that share a unit leave
+// partial sums in global memory, slice by slice, and the last to arrive joins them.  Every order is fixed: results are bit-reproducible.
+#include <cooperative_groups.h>
+
+#include <mutex>
+
+#include "decode_fold.cuh"
 #include "paged.cuh"
+
 namespace sc {
-bool paged_decode_mma_supported(const PagedDecodeArgs&) { return false; }
-cudaError_t launch_paged_decode_mma(const PagedDecodeArgs&, cudaStream_t) { return cudaErrorNotSupported; }
-size_t paged_decode_mma_ws_bytes() { return 0; }
+namespace pg {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+typedef __nv_bfloat16 bf16;
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kTile = 16;
+constexpr int kHeads = 8;                 // query heads at a time
+constexpr float kMaxSlack = 8.f;          // log2 units a score may exceed the running maximum before it is raised
+constexpr int kMaxBlocks = 320;           // of a launch
+constexpr int kMergeGroup = 8;            // partial sums read together
+constexpr unsigned kShortStretch = 64;    // tiles per block below which stretches are cut at the units' ends
+constexpr int kLeastShared = 2, kLeastAlone = 2;   // tiles per warp that a stretch of a cluster, or of a block, has at least
+
+template <int D>
+struct Shape {
+    static constexpr int kStages = D == 64 ? 6 : 3;                  // about 96 KB on their way per block (192 for d = 256)
+    static constexpr int kBlocksPerSm = D == 256 ? 1 : 2;
+    static constexpr int kRowBytes = D * 2;
+    static constexpr int kTileBytes = kTile * kRowBytes;             // of K or V
+    static constexpr int kStageBytes = 2 * kTileBytes + 80;          // K, V, 16 counts, which rows count
+    static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
+    static constexpr int kRecvO = (kHeads * (D / 4) + dm::kMaxCluster) * 16;   // slices of O from a cluster's blocks, rounded up
+    static constexpr int kRecvBytes = kRecvO + dm::kMaxCluster * kHeads * 8;   // and m, l
+    static constexpr int kSmemBytes = kRingBytes + 2 * kRecvBytes;
+    static constexpr int kPartStride = kHeads * D + 2 * kHeads;      // floats: acc[8][D], m[8], l[8]
+    static_assert(kWarps * kHeads * D * 4 <= kRingBytes, "the warps' sums lie in the ring's place");
+};
+static_assert(kMaxBlocks * 4 <= (int)kTicketBytes, "a counter per party and slice");
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int src_bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ float fast_log2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void store_out4(bf16* dst, const float4& o, float l) {   // (no row: zeros; l not a number: not a number)
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    const uint2 w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(dst) = w;
+}
+
+// One head's rows as a warp copies them: tile after tile into stages.
+template <int D, bool kWhole>
+struct Rows {
+    const bf16* k; const bf16* v;      // of the head inside the pages
+    const int32_t* count;              // likewise, or NULL
+    const int32_t* table;
+    const void* nowhere;               // a valid address for copies of no bytes
+    int64_t page_stride, row_stride;
+    int64_t count_page;
+    int num_pages, page_size, len;
+    int32_t* status;
+
+    // Pages are looked up for kBatch of the warp's tiles at a time (its j-th is tile first + j * kWarps), a batch ahead: one load, whose latency
+    // is longer than a tile takes.  kWhole (page_size a multiple of 16: a tile lies in one page): lane l has the batch's l-th tile; else the
+    // row lane & 15 of its (l / 16)-th.  x: the page, -1: no such row;  y: the row's (the tile's first row's) place in it.
+    static constexpr int kBatch = kWhole ? 32 : 2;
+    __device__ __forceinline__ int2 look_up(int first, int j0, int n, int lane) const {
+        const int j = j0 + (kWhole ? lane : lane >> 4);
+        int2 at = make_int2(-1, 0);
+        if (j >= n) return at;
+        const int row = (first + j * kWarps) * kTile + (kWhole ? 0 : lane & 15);
+        if (row < len) {
+            const int slot = row / page_size;
+            at = make_int2(table[slot], row - slot * page_size);
+        }
+        return at;
+    }
+    __device__ __forceinline__ int2 of_batch(const int2& batch, int j, int lane) const {
+        const int src = kWhole ? j & 31 : (j & 1) * 16 + (lane & 15);
+        return make_int2(__shfl_sync(kFull, batch.x, src), __shfl_sync(kFull, batch.y, src));
+    }
+    __device__ __forceinline__ void copy(uint32_t stage, int tile, int2 at, int lane) const {
+        constexpr int kChunks = D / 8, kStep = 32 / kChunks, kN = kTile / kStep;   // lanes per row, rows per round, rounds
+        using S = Shape<D>;
+        const int c = lane % kChunks, r0 = lane / kChunks;
+        const bool page = (unsigned)at.x < (unsigned)num_pages;
+        const uint32_t dst = stage + r0 * S::kRowBytes;
+        unsigned rows_ok;
+        if (kWhole) {
+            const int rows = page ? min(kTile, len - tile * kTile) : 0;
+            rows_ok = (1u << rows) - 1;
+            const int64_t first = at.x * page_stride + (int64_t)(at.y + r0) * row_stride + c * 8;
+            if (rows == kTile) {
+                const bf16* ks = k + first;
+                const bf16* vs = v + first;
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
+                    cp_async16(to, ks, 16);
+                    cp_async16(to + S::kTileBytes, vs, 16);
+                    ks += kStep * row_stride; vs += kStep * row_stride;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
+                    const bool ok = i * kStep + r0 < rows;
+                    const int64_t o = first + (int64_t)i * kStep * row_stride;
+                    cp_async16(to, ok ? (const void*)(k + o) : nowhere, ok ? 16 : 0);
+                    cp_async16(to + S::kTileBytes, ok ? (const void*)(v + o) : nowhere, ok ? 16 : 0);
+                }
+            }
+        } else {
+            const int64_t mine = page ? at.x * page_stride + (int64_t)at.y * row_stride : -1;
+            rows_ok = __ballot_sync(kFull, page) & 0xffff;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
+                const int64_t o = __shfl_sync(kFull, mine, i * kStep + r0);
+                cp_async16(to, o >= 0 ? (const void*)(k + o + c * 8) : nowhere, o >= 0 ? 16 : 0);
+                cp_async16(to + S::kTileBytes, o >= 0 ? (const void*)(v + o + c * 8) : nowhere, o >= 0 ? 16 : 0);
+            }
+        }
+        if (count != nullptr && lane < kTile) {
+            const bool ok = rows_ok >> lane & 1;
+            const int64_t o = at.x * count_page + at.y + (kWhole ? lane : 0);
+            cp_async4(stage + 2 * S::kTileBytes + lane * 4, ok ? (const void*)(count + o) : nowhere, ok ? 4 : 0);
+        }
+        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;\n" ::"r"(stage + 2 * S::kTileBytes + 64), "r"(rows_ok) : "memory");
+        if (!page && tile * kTile + (kWhole ? 0 : lane & 15) < len) set_status(status, SC_ERR_INVALID_ARG);
+    }
+};
+
+// kPair: up to four query heads (see above).
+template <int D, bool kWhole, bool kPair>
+__global__ void __launch_bounds__(kThreads, Shape<D>::kBlocksPerSm)
+paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int Hq, int Hkv, Line line, unsigned short_below, float scale_log2,
+                 bf16* __restrict__ out, int32_t* __restrict__ tickets, float* __restrict__ part, int32_t* status) {
+    using S = Shape<D>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float sh_m[kWarps][kHeads], sh_l[kWarps][kHeads];
+    __shared__ int sh_last;
+    __shared__ __align__(8) unsigned long long sh_bar[2];   // what the cluster's blocks hand this one, segments by turns
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, tig = lane & 3;
+    int csize = (int)cg::this_cluster().num_blocks(), crank = (int)cg::this_cluster().block_rank(), party = blockIdx.x / csize;
+    if (csize > 1) {
+        if (threadIdx.x == 0) {
+            umma::mbar_init(smem_u32(&sh_bar[0]), 1);
+            umma::mbar_init(smem_u32(&sh_bar[1]), 1);
+            umma::mbar_fence_init();
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // (waited for before the first hand-over)
+    }
+    in_stream_order();
+
+    const int G = Hq / Hkv, groups = (G + kHeads - 1) / kHeads;
+    const auto head_of = [&](int entry, int unit, int& b, int& h, int& g0) {
+        b = entry / pages.table_heads;
+        h = pages.table_heads > 1 ? entry - b * pages.table_heads : unit / groups;
+        g0 = unit % groups * kHeads;
+    };
+    const auto zero_empty = [&] {   // heads without rows
+        for (int e = blockIdx.x; e < line.entries; e += gridDim.x) {
+            if (line.len(e) > 0) continue;
+            for (int i = threadIdx.x; i < line.per_entry * kHeads * (D / 4); i += kThreads) {
+                int b, h, g0;
+                const int g1 = i / (D / 4) % kHeads;
+                head_of(e, i / (kHeads * (D / 4)), b, h, g0);
+                if (g0 + g1 < G) store_out4(out + ((int64_t)b * Hq + h * G + g0 + g1) * D + i % (D / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
+            }
+        }
+    };
+    unsigned total = total_of(line, lane);
+    bool in_step = csize == 1;   // the cluster's blocks are known to have started
+    if (total < short_below) {   // each block for itself (see start())
+        if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        in_step = true;
+        csize = 1; crank = 0; party = blockIdx.x;
+        line.parties = gridDim.x;
+    }
+    const unsigned least = csize * kWarps * (csize > 1 ? kLeastShared : kLeastAlone);
+    const unsigned stretch = max((total + line.parties - 1) / line.parties, least);
+    const bool cut = stretch < kShortStretch * csize && line.entries <= 64 && line.entries * line.per_entry <= line.parties;   // at the units' ends
+    Part own = {0, 0, 0, 0, 0, 0};
+    unsigned from = 0, left;
+    if (cut) {
+        own = part_of(line, stretch, party, lane);
+        left = own.take;
+    } else {
+        from = min((uint64_t)party * stretch, (uint64_t)total);
+        left = min(stretch, total - from);
+    }
+    if (left == 0) {
+        zero_empty();
+        if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        return;
+    }
+    bool got = true;             // no wait has given up
+    unsigned turn = 0;           // of the segment: which barrier, and its phase
+
+    // per-lane ldmatrix row/chunk selectors
+    const int lm_j = lane >> 3, lm_r = lane & 7;
+    const int k_row = lm_r + ((lm_j & 1) << 3), k_csel = lm_j >> 1;    // K: matrices (r0-7,c), (r8-15,c), (r0-7,c+1), (r8-15,c+1)
+    const int v_row = lm_r + ((lm_j >> 1) << 3), v_csel = lm_j & 1;    // V^T: (r0-7,c), (r0-7,c+1), (r8-15,c), (r8-15,c+1)
+    const uint32_t ring = smem_u32(smem) + warp * (S::kStages * S::kStageBytes);
+
+    for (Place p = cut ? Place{own.entry, own.unit, own.tile, 0u} : place_of(line, from, lane);;) {
+        const int len = line.len(p.entry), nt = line.tiles(p.entry);
+        const int take = (int)min((unsigned)(nt - p.tile), left);
+        int b, h, g0;
+        head_of(p.entry, p.unit, b, h, g0);
+        const int nh = min(kHeads, G - g0);
+        const int64_t hq0 = (int64_t)b * Hq + h * G + g0;
+        // this block's tiles of the segment, and this warp's: t0 + warp, t0 + warp + kWarps, ...
+        const int each = (take + csize - 1) / csize, t0 = p.tile + min(crank * each, take), t1 = p.tile + min((crank + 1) * each, take);
+        const int my_tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
+        Rows<D, kWhole> rows;
+        {
+            const int hp = pages.page_heads > 1 ? h : 0;
+            rows.k = pages.k + hp * pages.head_stride; rows.v = pages.v + hp * pages.head_stride;
+            rows.count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
+            rows.count_page = (int64_t)pages.page_heads * pages.page_size;
+            rows.table = pages.table_of(p.entry); rows.nowhere = q;
+            rows.page_stride = pages.page_stride; rows.row_stride = pages.row_stride;
+            rows.num_pages = pages.num_pages; rows.page_size = pages.page_size; rows.len = len; rows.status = status;
+        }
+        int2 batch = rows.look_up(t0 + warp, 0, my_tiles, lane), next_batch = rows.look_up(t0 + warp, rows.kBatch, my_tiles, lane);
+        const auto copy = [&](uint32_t stage, int j) {   // the warp's j-th tile, j = 0, 1, ...
+            if (j % rows.kBatch == 0 && j > 0) {
+                batch = next_batch;
+                next_batch = rows.look_up(t0 + warp, j + rows.kBatch, my_tiles, lane);
+            }
+            rows.copy(stage, t0 + warp + j * kWarps, rows.of_batch(batch, j, lane), lane);
+        };
+#pragma unroll
+        for (int s = 0; s < S::kStages; ++s) {
+            if (s < my_tiles) copy(ring + s * S::kStageBytes, s);
+            cp_async_commit();
+        }
+        // q^T as the B operand of every k-step: b0 = q[head g][16ks + 2tig, +1], b1 = same + 8
+        uint32_t qb[D / 16][2];
+        {
+            const int hd = kPair ? g & 3 : g;
+            const bf16* qh = q + (hq0 + hd) * D + 2 * tig;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                qb[ks][0] = hd < nh ? *reinterpret_cast<const uint32_t*>(qh + ks * 16) : 0u;
+                qb[ks][1] = hd < nh ? *reinterpret_cast<const uint32_t*>(qh + ks * 16 + 8) : 0u;
+            }
+        }
+        float o[D / 16][4];
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt) { o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f; }
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // columns 2tig and 2tig+1
+
+        int at_stage = 0;
+        for (int i = 0; i < my_tiles; ++i) {
+            cp_async_wait<S::kStages - 1>();   // tile i has landed, the next ones are on their way
+            __syncwarp();
+            const uint32_t st = ring + at_stage * S::kStageBytes;
+            const unsigned char* st_p = smem + warp * (S::kStages * S::kStageBytes) + at_stage * S::kStageBytes;
+
+            // S^T = K . q^T, four accumulator chains
+            float s[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                uint32_t a[4];
+                const int c = 2 * ks + k_csel;
+                ldmatrix_x4(st + k_row * S::kRowBytes + ((c ^ (k_row & 7)) << 4), a);
+                mma_bf16(s[ks & 3], a, qb[ks][0], qb[ks][1]);
+            }
+            const unsigned rows_ok = *reinterpret_cast<const unsigned*>(st_p + 2 * S::kTileBytes + 64);
+            float lc_lo = 0.f, lc_hi = 0.f;
+            if (rows.count != nullptr) {
+                const int* cs = reinterpret_cast<const int*>(st_p + 2 * S::kTileBytes);
+                lc_lo = fast_log2((float)max(cs[g], 1));
+                lc_hi = fast_log2((float)max(cs[g + 8], 1));
+            }
+            const bool ok_lo = rows_ok >> g & 1, ok_hi = rows_ok >> (g + 8) & 1;
+            const float x0 = ok_lo ? fmaf((s[0][0] + s[1][0]) + (s[2][0] + s[3][0]), scale_log2, lc_lo) : -INFINITY;
+            const float x1 = ok_lo ? fmaf((s[0][1] + s[1][1]) + (s[2][1] + s[3][1]), scale_log2, lc_lo) : -INFINITY;
+            const float x2 = ok_hi ? fmaf((s[0][2] + s[1][2]) + (s[2][2] + s[3][2]), scale_log2, lc_hi) : -INFINITY;
+            const float x3 = ok_hi ? fmaf((s[0][3] + s[1][3]) + (s[2][3] + s[3][3]), scale_log2, lc_hi) : -INFINITY;
+            const float lx0 = fmaxf(x0, x2), lx1 = fmaxf(x1, x3);
+            if (__any_sync(kFull, (lx0 > m0 + kMaxSlack) || (lx1 > m1 + kMaxSlack))) {
+                float mx0 = lx0, mx1 = lx1;
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) {
+                    mx0 = fmaxf(mx0, __shfl_xor_sync(kFull, mx0, off));
+                    mx1 = fmaxf(mx1, __shfl_xor_sync(kFull, mx1, off));
+                }
+                const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
+                const float c0 = mn0 == -INFINITY ? 1.f : dm::fast_exp2(m0 - mn0), c1 = mn1 == -INFINITY ? 1.f : dm::fast_exp2(m1 - mn1);
+                l0 *= c0; l1 *= c1;
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt) { o[mt][0] *= c0; o[mt][2] *= c0; o[mt][1] *= c1; o[mt][3] *= c1; }
+                m0 = mn0; m1 = mn1;
+            }
+            const float e0 = m0 == -INFINITY ? 0.f : m0, e1 = m1 == -INFINITY ? 0.f : m1;   // (a tile whose page does not exist has no row)
+            const float w0 = dm::fast_exp2(x0 - e0), w1 = dm::fast_exp2(x1 - e1);   // row g
+            const float w2 = dm::fast_exp2(x2 - e0), w3 = dm::fast_exp2(x3 - e1);   // row g + 8
+            const uint32_t p_lo = pack_bf16x2(w0, w1), p_hi = pack_bf16x2(w2, w3);
+            const uint32_t r_lo = pack_bf16x2(w0 - bf16_lo(p_lo), w1 - bf16_hi(p_lo));
+            const uint32_t r_hi = pack_bf16x2(w2 - bf16_lo(p_hi), w3 - bf16_hi(p_hi));
+            l0 += (bf16_lo(p_lo) + bf16_lo(r_lo)) + (bf16_lo(p_hi) + bf16_lo(r_hi));
+            l1 += (bf16_hi(p_lo) + bf16_hi(r_lo)) + (bf16_hi(p_hi) + bf16_hi(r_hi));
+            const uint32_t pb0 = movmatrix_trans(kPair && tig >= 2 ? r_lo : p_lo), pb1 = movmatrix_trans(kPair && tig >= 2 ? r_hi : p_hi);
+            const uint32_t rb0 = kPair ? 0u : movmatrix_trans(r_lo), rb1 = kPair ? 0u : movmatrix_trans(r_hi);
+
+            // O^T += V^T . P^T
+#pragma unroll
+            for (int mt = 0; mt < D / 16; ++mt) {
+                uint32_t a[4];
+                const int c = 2 * mt + v_csel;
+                ldmatrix_x4_trans(st + S::kTileBytes + v_row * S::kRowBytes + ((c ^ (v_row & 7)) << 4), a);
+                mma_bf16(o[mt], a, pb0, pb1);
+                if (!kPair) mma_bf16(o[mt], a, rb0, rb1);
+            }
+            __syncwarp();
+            // the stage just consumed takes the next tile
+            if (i + S::kStages < my_tiles) copy(st, i + S::kStages);
+            cp_async_commit();
+            at_stage = at_stage + 1 == S::kStages ? 0 : at_stage + 1;
+        }
+        cp_async_wait<0>();
+
+        // ---- the warps of this block meet (fixed order) ----
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {   // lane-local l covers rows g, g+8 of every tile
+            l0 += __shfl_xor_sync(kFull, l0, off);
+            l1 += __shfl_xor_sync(kFull, l1, off);
+        }
+        if (g == 0) {
+            sh_m[warp][2 * tig] = m0; sh_m[warp][2 * tig + 1] = m1;
+            sh_l[warp][2 * tig] = l0; sh_l[warp][2 * tig + 1] = l1;
+        }
+        __syncthreads();   // every warp is done with its ring; reuse it as [warp][8 columns][D] fp32
+        float bm0 = -INFINITY, bm1 = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) { bm0 = fmaxf(bm0, sh_m[w][2 * tig]); bm1 = fmaxf(bm1, sh_m[w][2 * tig + 1]); }
+        const float f0 = m0 == -INFINITY ? 0.f : dm::fast_exp2(m0 - bm0), f1 = m1 == -INFINITY ? 0.f : dm::fast_exp2(m1 - bm1);
+        float* slabs = reinterpret_cast<float*>(smem);
+        float* slab = slabs + warp * (kHeads * D);
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt) {
+            const int d0 = mt * 16 + g;
+            slab[(2 * tig) * D + d0] = o[mt][0] * f0;
+            slab[(2 * tig + 1) * D + d0] = o[mt][1] * f1;
+            slab[(2 * tig) * D + d0 + 8] = o[mt][2] * f0;
+            slab[(2 * tig + 1) * D + d0 + 8] = o[mt][3] * f1;
+        }
+        __syncthreads();
+        const auto block_sum = [&](int e4) {   // four columns of a head: e4 = head * D / 4 + column / 4
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float4 v = *reinterpret_cast<const float4*>(slabs + w * (kHeads * D) + e4 * 4);
+                acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+                if (kPair) {   // the remainders' part
+                    const float4 r = *reinterpret_cast<const float4*>(slabs + w * (kHeads * D) + 4 * D + e4 * 4);
+                    acc.x += r.x; acc.y += r.y; acc.z += r.z; acc.w += r.w;
+                }
+            }
+            return acc;
+        };
+        const auto block_ml = [&](int hd) {
+            float bm = -INFINITY, bl = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) bm = fmaxf(bm, sh_m[w][hd]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) bl += sh_m[w][hd] == -INFINITY ? 0.f : sh_l[w][hd] * dm::fast_exp2(sh_m[w][hd] - bm);
+            return make_float2(bm, bl);
+        };
+        const bool whole = take == nt;
+        const int n4 = nh * (D / 4), slice = (n4 + csize - 1) / csize, e_lo = min(crank * slice, n4), e_hi = min(e_lo + slice, n4);
+        float* mine = part + (size_t)(2 * party + (!cut && p.at > from)) * S::kPartStride;
+        const auto give = [&](int e4, const float4& acc, float m, float l) {
+            const int hd = e4 / (D / 4), d4 = e4 % (D / 4) * 4;
+            if (whole) {
+                store_out4(out + (hq0 + hd) * D + d4, acc, l);
+            } else {
+                *reinterpret_cast<float4*>(mine + hd * D + d4) = acc;
+                if (d4 == 0 || e4 == e_lo) { mine[kHeads * D + hd] = m; mine[kHeads * D + kHeads + hd] = l; }   // (the same from every slice of the head)
+            }
+        };
+        if (csize == 1) {
+            for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
+                const float2 ml = block_ml(e4 / (D / 4));
+                give(e4, block_sum(e4), ml.x, ml.y);
+            }
+        } else {
+            // Every block hands slice r of its sums to block r, which folds it.  A block's receiving places are used by turns: who hands it
+            // something for the segment after the next has its slice of the next one, so it is done with this one.
+            const uint32_t bar = smem_u32(&sh_bar[turn & 1]);
+            unsigned char* recv = smem + S::kRingBytes + (turn & 1) * S::kRecvBytes;
+            float4* recv_o = reinterpret_cast<float4*>(recv);
+            float* recv_ml = reinterpret_cast<float*>(recv + S::kRecvO);
+            if (threadIdx.x == 0) umma::mbar_expect_tx(bar, (uint32_t)(csize * ((e_hi - e_lo) * 16 + kHeads * 8)));
+            if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // every block of the cluster has started
+            in_step = true;
+            for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
+                const int to = e4 / slice;
+                dm::hand_over(dm::mapa(smem_u32(recv_o + crank * slice + (e4 - to * slice)), to), dm::mapa(bar, to), block_sum(e4));
+            }
+            for (int x = threadIdx.x; x < csize * kHeads; x += kThreads) {
+                const float2 ml = block_ml(x & 7);
+                dm::hand_over(dm::mapa(smem_u32(recv_ml + crank * 2 * kHeads + (x & 7) * 2), x >> 3), dm::mapa(bar, x >> 3), ml.x, ml.y);
+            }
+            if (got) got = umma::mbar_wait<true>(bar, turn >> 1 & 1);
+            if (!got) set_status(status, SC_ERR_TIMEOUT);
+            for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
+                const dm::Folded f = dm::fold_slices(recv_o, recv_ml, csize, slice, e4 - e_lo, e4 / (D / 4), got);
+                give(e4, f.o, f.m, f.l);
+            }
+            ++turn;
+        }
+        if (!whole) {
+            // Parties that share a unit: the last one to bring a slice joins the slice's parts in order.
+            const unsigned first = cut ? party - own.index : p.at / stretch, last = cut ? first + own.parts - 1 : (p.at + nt - 1) / stretch;
+            int32_t* ticket = tickets + (first * csize + crank);   // (a party begins one shared unit at most)
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                int t;
+                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(t) : "l"(ticket) : "memory");
+                sh_last = t == (int)(last - first);
+                if (sh_last) *ticket = 0;   // ready for the next call
+            }
+            __syncthreads();
+            if (sh_last) {
+                for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
+                    const int hd = e4 / (D / 4), d4 = e4 % (D / 4) * 4;
+                    float m = -INFINITY, l = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (unsigned j0 = first; j0 <= last; j0 += kMergeGroup) {
+                        float mv[kMergeGroup], lv[kMergeGroup];
+                        float4 ov[kMergeGroup];
+#pragma unroll
+                        for (int j = 0; j < kMergeGroup; ++j) {
+                            const bool ok = j0 + j <= last;
+                            const unsigned w = ok ? j0 + j : first;
+                            const float* sp = part + (size_t)(2 * w + (!cut && p.at > w * stretch)) * S::kPartStride;
+                            mv[j] = ok ? __ldcg(sp + kHeads * D + hd) : -INFINITY;
+                            lv[j] = __ldcg(sp + kHeads * D + kHeads + hd);
+                            ov[j] = __ldcg(reinterpret_cast<const float4*>(sp + hd * D + d4));
+                        }
+                        float nm = m;
+#pragma unroll
+                        for (int j = 0; j < kMergeGroup; ++j) nm = fmaxf(nm, mv[j]);
+                        if (nm == -INFINITY) continue;   // nothing but parts without rows so far
+                        const float c = m == -INFINITY ? 0.f : dm::fast_exp2(m - nm);
+                        l *= c; acc.x *= c; acc.y *= c; acc.z *= c; acc.w *= c;
+                        m = nm;
+#pragma unroll
+                        for (int j = 0; j < kMergeGroup; ++j) {
+                            if (mv[j] == -INFINITY) continue;
+                            const float w = dm::fast_exp2(mv[j] - m);
+                            l = fmaf(w, lv[j], l);
+                            acc.x = fmaf(w, ov[j].x, acc.x); acc.y = fmaf(w, ov[j].y, acc.y);
+                            acc.z = fmaf(w, ov[j].z, acc.z); acc.w = fmaf(w, ov[j].w, acc.w);
+                        }
+                    }
+                    store_out4(out + (hq0 + hd) * D + d4, acc, l);
+                }
+            }
+        }
+        left -= take;
+        if (left == 0) break;
+        next_unit(line, p, nt);
+        __syncthreads();   // the ring, sh_m and sh_l are written again
+    }
+    zero_empty();
+    if (csize > 1 && !__all_sync(kFull, got)) {
+        // Gave up on a hand-over: the block's shared memory stays until the cluster's other blocks have left (each of their waits ends, and a
+        // thread that has left is not waited for) and what they handed over has landed.
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        for (unsigned back = 1; back <= 2 && back <= turn; ++back) umma::mbar_wait<true>(smem_u32(&sh_bar[(turn - back) & 1]), (turn - back) >> 1 & 1);
+    }
+}
+
+template <int D, bool kWhole, bool kPair>
+cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStream_t st) {
+    static std::once_flag once[64];   // per device
+    static cudaError_t ready[64];
+    std::call_once(once[dev & 63], [dev] {
+        ready[dev & 63] = own_error(cudaFuncSetAttribute(paged_decode_mma<D, kWhole, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmemBytes));
+    });
+    if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
+    const int64_t units = (int64_t)line.entries * line.per_entry;
+    int blocks = sms * Shape<D>::kBlocksPerSm;
+    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    // Up to 64 units: clusters of four, as many as find room at once (7/8 of the block slots: 64 of 4 x 74), and of those a multiple of the units
+    // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.0
+    // and 17, of 32 K 31.0 and 38.0, of 128 K 98 and 102; 4 units of 128 K with seven query heads 55 and 74; 16 units of 32 K 53 and 58.  Clusters
+    // of eight: 1 K rows 7.8 and 9.8 (of four), but 8 K 15.7 and 13.2, because the next launch's clusters find room only when this one is gone.
+    // From 17 units on each block stands for itself where the units are short: 32 units of 3 K rows 18.3 (clusters 21), of 25 K 81 and 81.
+    // More units: single blocks (128 units of 150 rows 12.8, in clusters of two 17.1; of 12 K rows 138 and 135; 512 of 1.5 K 73.5 and 76.2).
+    const int c = units <= 64 ? 4 : 1;
+    unsigned short_below = 0;
+    line.parties = blocks;
+    if (c > 1) {
+        line.parties = blocks * 7 / 8 / c;
+        if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
+        short_below = units <= 16 ? 0 : (unsigned)units * 512;
+    }
+    const float scale = (a.scale == 0.f ? 1.f / sqrtf((float)a.d) : a.scale) * 1.4426950408889634f;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(line.parties * c);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = c > 1 ? Shape<D>::kSmemBytes : Shape<D>::kRingBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return own_error(cudaLaunchKernelEx(&cfg, paged_decode_mma<D, kWhole, kPair>, pages_of<const bf16>(a.cache), (const bf16*)a.q, a.Hq, a.Hkv, line, short_below,
+                                        scale, (bf16*)a.out, (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status));
+}
+
+template <int D>
+cudaError_t start(const PagedDecodeArgs& a, const Line& line, int dev, int sms, cudaStream_t st) {
+    const bool whole = a.cache.page_size % kTile == 0, pair = a.Hq / a.Hkv <= 4;
+    return whole ? (pair ? start<D, true, true>(a, line, dev, sms, st) : start<D, true, false>(a, line, dev, sms, st))
+                 : (pair ? start<D, false, true>(a, line, dev, sms, st) : start<D, false, false>(a, line, dev, sms, st));
+}
+
+}  // namespace
+
+}  // namespace pg
+
+bool paged_decode_mma_supported(const PagedDecodeArgs& a) { return a.dt == SC_BF16 && (a.d == 64 || a.d == 128 || a.d == 256); }
+
+size_t paged_decode_mma_ws_bytes() { return pg::kTicketBytes + sizeof(float) * 2 * pg::kMaxBlocks * pg::Shape<256>::kPartStride; }
+
+cudaError_t launch_paged_decode_mma(const PagedDecodeArgs& a, cudaStream_t st) {
+    int dev = 0, sms = 148;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    pg::Line line;
+    line.lens = a.lens; line.entries = a.B * a.cache.table_heads;
+    line.per_entry = a.Hkv / a.cache.table_heads * div_up(a.Hq / a.Hkv, pg::kHeads);
+    line.cap = a.cache.max_pages * a.cache.page_size; line.tile = pg::kTile;
+    const cudaError_t e = a.d == 64 ? pg::start<64>(a, line, dev, sms, st) : a.d == 128 ? pg::start<128>(a, line, dev, sms, st) : pg::start<256>(a, line, dev, sms, st);
+    if (e == cudaSuccess) note_launches(1);
+    return e;
+}
+
+}  // namespace sc

@@ -50,14 +50,12 @@ paged_decode_generic(const Pages<T> pages, const T* __restrict__ q, int Hq, int 
             if (g0 + g < G) Elem<T>::store(out + ((int64_t)b * Hq + h * G + g0 + g) * d + i % d, 0.f);
         }
     }
-    int64_t total;
-    const int64_t stretch = stretch_of(line, kLeast, lane, total);
-    const int64_t from = blockIdx.x * stretch;
+    const unsigned total = total_of(line, lane), stretch = max((total + line.parties - 1) / line.parties, (unsigned)kLeast), from = min((uint64_t)blockIdx.x * stretch, (uint64_t)total);
     if (from >= total) return;
-    int64_t left = min(stretch, total - from);
+    unsigned left = min(stretch, total - from);
     for (Place p = place_of(line, from, lane);;) {
         const int len = line.len(p.entry), nt = line.tiles(p.entry);
-        const int take = (int)min((int64_t)(nt - p.tile), left), t_end = p.tile + take;
+        const int take = (int)min((unsigned)(nt - p.tile), left), t_end = p.tile + take;
         int b, h, g0;
         head_of(p.entry, p.unit, b, h, g0);
         const int nh = min(kHeads, G - g0), hq0 = b * Hq + h * G + g0;
@@ -177,7 +175,7 @@ paged_decode_generic(const Pages<T> pages, const T* __restrict__ q, int Hq, int 
         __syncthreads();
         const bool whole = take == nt;
         const int part_stride = kHeads * (d + 2);
-        float* mine = part + (2ll * blockIdx.x + (p.at > from)) * part_stride;   // [head][d columns, m, l]
+        float* mine = part + (size_t)(2 * blockIdx.x + (p.at > from)) * part_stride;   // [head][d columns, m, l]
         for (int i = threadIdx.x; i < nh * d; i += kWarps * 32) {
             const int g = i / d, c = i - g * d;
             float mm = -INFINITY;
@@ -198,7 +196,7 @@ paged_decode_generic(const Pages<T> pages, const T* __restrict__ q, int Hq, int 
             }
         }
         if (!whole) {
-            const int64_t first = p.at / stretch, last = (p.at + nt - 1) / stretch;
+            const unsigned first = p.at / stretch, last = (p.at + nt - 1) / stretch;
             int32_t* ticket = tickets + first;   // (a party begins one shared unit at most)
             __threadfence();
             __syncthreads();
@@ -213,8 +211,8 @@ paged_decode_generic(const Pages<T> pages, const T* __restrict__ q, int Hq, int 
                 for (int i = threadIdx.x; i < nh * d; i += kWarps * 32) {
                     const int g = i / d, c = i - g * d;
                     float mm = -INFINITY, ls = 0.f, o = 0.f;
-                    for (int64_t j = first; j <= last; ++j) {
-                        const float* from_j = part + (2 * j + (p.at > j * stretch)) * part_stride + g * (d + 2);
+                    for (unsigned j = first; j <= last; ++j) {
+                        const float* from_j = part + (size_t)(2 * j + (p.at > j * stretch)) * part_stride + g * (d + 2);
                         const float mj = __ldcg(from_j + d), lj = __ldcg(from_j + d + 1), oj = __ldcg(from_j + c);
                         const float mn = fmaxf(mm, mj), ref = mn == -INFINITY ? 0.f : mn;
                         const float c0 = exp2f(mm - ref), c1 = exp2f(mj - ref);

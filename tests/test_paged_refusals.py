@@ -115,6 +115,12 @@ def test_select_needs_bounds_and_tables_it_can_hold(lib):
     assert select(lib, _cache(max_pages=many, table_stride=many)) == UNSUPPORTED
 
 
+def test_more_rows_than_a_launch_can_number(lib):
+    wide = dict(max_pages=2 ** 26, table_stride=2 ** 26)
+    assert decode(lib, _cache(**wide), B=4, Hq=32, Hkv=8) == UNSUPPORTED      # 4 * 8 heads x 2^26 tiles of 16 rows
+    assert decode(lib, _cache(**wide, page_heads=2), B=1, Hq=128, Hkv=2) == UNSUPPORTED   # 2 heads x 16 groups of queries
+
+
 def test_nothing_to_do(lib):
     """No sequences: fine without any pointer but the structures."""
     empty = _cache(k=None, v=None, num_pages=0, table=None, max_pages=0, k_min=None, k_max=None)
