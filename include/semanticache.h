@@ -444,9 +444,9 @@ typedef struct {
  * prompts, single generated tokens, or both.
  *
  * The rotation (inv_freq not NULL) turns each pair (x1, x2) of the first rot_dim columns of a key or query by the angle
- * a_i = position * inv_freq[i]:  y1 = x1 cos a_i - x2 sin a_i,  y2 = x2 cos a_i + x1 sin a_i.  The angle is taken in 64
- * bits, so far positions lose nothing; products in fp32, one rounding to dt.  Values and the columns behind rot_dim
- * are copied.
+ * a_i = position * inv_freq[i]:  y1 = x1 cos a_i - x2 sin a_i,  y2 = x2 cos a_i + x1 sin a_i.  The angle is taken in 64-bit
+ * fractions of a turn, so far positions lose nothing; products in fp32, one rounding to dt.  Values and the columns behind
+ * rot_dim are copied.
  *
  *   rows (HOST)
  *     k, v        [T, Hkv, d], dtype dt, element strides kv_token, kv_head (16-byte multiples; d contiguous)
@@ -459,7 +459,7 @@ typedef struct {
  *                 a model append at the same place, so the lengths move on once per step, not once per call.
  *     q, q_out    [T, Hq, d] queries of the same tokens and where they go rotated; both NULL to skip.  Element strides
  *                 q_token, q_head and qo_token, qo_head (16-byte multiples); q_out may be q itself.
- *     inv_freq    [rot_dim / 2] float (device), or NULL: no rotation;  rot_dim even, 0..d
+ *     inv_freq    [rot_dim / 2] float (device), finite, of magnitude below 2^40, or NULL: no rotation;  rot_dim even, 0..d
  *     positions   [T] int32 (device), or NULL: a token's position is the row it gets
  *   cache       its tables are [B, 1, max_pages] and its pages hold all Hkv heads.  A cache with tables and pages per head is
  *               appended to as B * Hkv sequences of one head each; so does the output of sc_compress get into pages: T =

@@ -595,7 +595,7 @@ class PagedCache:
             raise ValueError("the parts of a cache live on one device")
         form = _PagedCache(None, None, _step(k, 0), _step(k, 1), k.stride(2) if ps > 1 else d, P, ps, heads, None, stride, th, W, None, None,
                            None)
-        for name, value in (("B", table.shape[0]), ("heads", heads), ("table_heads", th), ("d", d), ("_dt", _dt(k)), ("_dev", dev),
+        for name, value in (("B", table.shape[0]), ("heads", heads), ("Hkv", heads if heads > 1 else th), ("table_heads", th), ("d", d), ("_dt", _dt(k)), ("_dev", dev),
                             ("_form", bytes(form))):
             object.__setattr__(self, name, value)
 
@@ -614,100 +614,110 @@ class PagedCache:
                 self._form)
 
 
-def _same_device(cache: PagedCache, *ts):
-    for t in ts:
-        if t is not None and t.get_device() != cache._dev:
-            raise ValueError("tensors of the cache's device required")
+def _lengths(t: torch.Tensor, n: int, dev: int, what: str):
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what}: {n} contiguous int32 on the cache's device")
 
 
-def _lengths(t: torch.Tensor, n: int, what: str):
-    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: {n} contiguous int32")
+def _heads_of_tokens(t: torch.Tensor, cache: PagedCache, what: str):
+    """Shape and element strides of rows [T, heads, d] of the cache's type (a stride is 0 where there is one entry)."""
+    if t.dim() != 3 or t.dtype is not cache.k.dtype or t.get_device() != cache._dev:
+        raise ValueError(f"{what}: [T, heads, d] of the cache's type, on its device")
+    T, H, d = t.shape
+    s0, s1, s2 = t.stride()
+    if d != cache.d or (s2 != 1 and T * H):
+        raise ValueError(f"{what}: [T, heads, {cache.d}], d contiguous")
+    return T, H, s0 if T > 1 else 0, s1 if H > 1 else 0
 
 
-def _called(name: str, dev: int, *args):
+def _called(fn, dev: int, args):
     """A call of the native extension with ``dev`` as the current device."""
-    fn = getattr(_native(), name)
-    if dev == torch.cuda.current_device():
-        code = fn(*args)
-    else:
-        with torch.cuda.device(dev):
-            code = fn(*args)
-    if code != SC_OK:
-        raise ScError("sc_" + name, code)
+    if dev == torch._C._cuda_getDevice():
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
 
 
 def sc_paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, seq_len=None, count_new=None, len_out=None, q=None, q_out=None,
                     inv_freq=None, positions=None, status=None, flags=0):
     """Raw sc_paged_append: rows k_new, v_new [T, Hkv, d] join the cache of their sequences (see the header).  ``inv_freq``
     (float32) turns the first 2 * len(inv_freq) columns of the keys, and of ``q`` [T, Hq, d] on its way to ``q_out``."""
-    _same_device(cache, k_new, v_new, seq_off, cache_len, seq_len, count_new, len_out, q, q_out, inv_freq, positions, status)
-    T, Hkv, d = k_new.shape
-    B = cache.B
-    if v_new.shape != k_new.shape or Hkv != cache.heads or d != cache.d:
-        raise ValueError("k_new and v_new: [T, heads, d] as the cache's pages")
-    ks = (_step(k_new, 0), _step(k_new, 1))
-    if k_new.stride(2) != 1 or v_new.stride(2) != 1 or ks != (_step(v_new, 0), _step(v_new, 1)):
-        raise ValueError("k_new and v_new: one layout, d contiguous")
-    if k_new.dtype != cache.k.dtype or v_new.dtype != cache.k.dtype:
-        raise TypeError("k_new and v_new must have the cache's type")
-    _lengths(seq_off, B + 1, "seq_off")
-    _lengths(cache_len, B, "cache_len")
-    for t, n, what in ((seq_len, B, "seq_len"), (len_out, B, "len_out"), (count_new, T * Hkv, "count_new"), (positions, T, "positions")):
-        if t is not None:
-            _lengths(t, n, what)
-    Hq, qs, qos = Hkv, (0, 0), (0, 0)
-    if (q is None) != (q_out is None):
+    dev, B = cache._dev, cache.B
+    T, Hkv, ks0, ks1 = rows = _heads_of_tokens(k_new, cache, "k_new")
+    if _heads_of_tokens(v_new, cache, "v_new") != rows:
+        raise ValueError("k_new and v_new: one shape and layout")
+    if Hkv != cache.heads:
+        raise ValueError("k_new and v_new: as many heads as a page of the cache")
+    _lengths(seq_off, B + 1, dev, "seq_off")
+    _lengths(cache_len, B, dev, "cache_len")
+    if seq_len is not None:
+        _lengths(seq_len, B, dev, "seq_len")
+    if len_out is not None:
+        _lengths(len_out, B, dev, "len_out")
+    if count_new is not None:
+        _lengths(count_new, T * Hkv, dev, "count_new")
+    if positions is not None:
+        _lengths(positions, T, dev, "positions")
+    Hq, qs0, qs1, qo0, qo1 = Hkv, 0, 0, 0, 0
+    if q is not None and q_out is not None:
+        Tq, Hq, qs0, qs1 = _heads_of_tokens(q, cache, "q")
+        To, Ho, qo0, qo1 = _heads_of_tokens(q_out, cache, "q_out")
+        if Tq != T or To != T or Ho != Hq:
+            raise ValueError("q and q_out: [T, Hq, d]")
+    elif q is not None or q_out is not None:
         raise ValueError("q and q_out go together")
-    if q is not None:
-        Hq = q.shape[1]
-        if q.shape != (T, Hq, d) or q_out.shape != q.shape or q.stride(2) != 1 or q_out.stride(2) != 1:
-            raise ValueError("q and q_out: [T, Hq, d], d contiguous")
-        if q.dtype != cache.k.dtype or q_out.dtype != cache.k.dtype:
-            raise TypeError("q and q_out must have the cache's type")
-        qs, qos = (_step(q, 0), _step(q, 1)), (_step(q_out, 0), _step(q_out, 1))
     rot = 0
     if inv_freq is not None:
-        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq: contiguous float32")
+        if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous() or inv_freq.get_device() != dev:
+            raise ValueError("inv_freq: contiguous float32 on the cache's device")
         rot = 2 * inv_freq.numel()
-    _called("paged_append", cache._dev, *cache._pointers(), k_new.data_ptr(), v_new.data_ptr(), *ks, _ptr(count_new), seq_off.data_ptr(),
-            _ptr(seq_len), cache_len.data_ptr(), _ptr(len_out), _ptr(q), _ptr(q_out), *qs, *qos, _ptr(inv_freq), rot, _ptr(positions),
-            cache._dt, B, Hq, Hkv, T, d, int(flags), _ptr(status), _stream(k_new))
+    code = _called(_native().paged_append, dev, (
+        *cache._pointers(), k_new.data_ptr(), v_new.data_ptr(), ks0, ks1, _ptr(count_new), seq_off.data_ptr(), _ptr(seq_len),
+        cache_len.data_ptr(), _ptr(len_out), _ptr(q), _ptr(q_out), qs0, qs1, qo0, qo1, _ptr(inv_freq), rot, _ptr(positions), cache._dt, B, Hq,
+        Hkv, T, cache.d, int(flags), _ptr(status), _stream(k_new)))
+    if code != SC_OK:
+        raise ScError("sc_paged_append", code)
+
+
+def _query(q: torch.Tensor, cache: PagedCache, what: str):
+    if q.dim() != 3 or q.dtype is not cache.k.dtype or not q.is_contiguous() or q.get_device() != cache._dev:
+        raise ValueError(f"{what}: contiguous [B, Hq, d] of the cache's type, on its device")
+    B, Hq, d = q.shape
+    if B != cache.B or d != cache.d:
+        raise ValueError(f"{what}: [{cache.B}, Hq, {cache.d}]")
+    return Hq
 
 
 def sc_paged_decode_attn(q, cache: PagedCache, lens, out, workspace, scale=0.0, status=None, flags=0):
     """Raw sc_paged_decode_attn: one decode step over a paged cache, q/out [B, Hq, d], lens int32 [B] or [B, table_heads]."""
-    _same_device(cache, q, lens, out, workspace, status)
-    B, Hq, d = q.shape
-    th = cache.table_heads
-    Hkv = cache.heads if cache.heads > 1 else th
-    if B != cache.B or d != cache.d or out.shape != q.shape or not q.is_contiguous() or not out.is_contiguous():
-        raise ValueError("q and out: contiguous [B, Hq, d] as the cache")
-    if q.dtype != cache.k.dtype or out.dtype != q.dtype:
-        raise TypeError("q and out must have the cache's type")
-    _lengths(lens, B * th, "lens")
-    _called("paged_decode_attn", cache._dev, *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, d, lens.data_ptr(), float(scale), int(flags),
-            out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(q))
+    dev, B = cache._dev, cache.B
+    Hq = _query(q, cache, "q")
+    if _query(out, cache, "out") != Hq:
+        raise ValueError("out: the shape of q")
+    _lengths(lens, B * cache.table_heads, dev, "lens")
+    if workspace.get_device() != dev:
+        raise ValueError("a workspace on the cache's device required")
+    code = _called(_native().paged_decode_attn, dev, (
+        *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, cache.Hkv, cache.d, lens.data_ptr(), float(scale), int(flags), out.data_ptr(),
+        workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(q)))
+    if code != SC_OK:
+        raise ScError("sc_paged_decode_attn", code)
 
 
 def sc_paged_select(q, cache: PagedCache, lens, keep, n_first, n_last, sel_table, sel_len, status=None):
     """Raw sc_paged_select: the ``keep`` pages of every (sequence, KV head) whose keys can score highest (see the header)."""
-    _same_device(cache, q, lens, sel_table, sel_len, status)
-    B, Hq, d = q.shape
-    th = cache.table_heads
-    Hkv = cache.heads if cache.heads > 1 else th
-    if B != cache.B or d != cache.d or not q.is_contiguous():
-        raise ValueError("q: contiguous [B, Hq, d] as the cache")
-    if q.dtype != cache.k.dtype:
-        raise TypeError("q must have the cache's type")
+    dev, B, Hkv = cache._dev, cache.B, cache.Hkv
+    Hq = _query(q, cache, "q")
     if cache.k_min is None:
         raise ValueError("a cache with k_min and k_max required")
-    _lengths(lens, B * th, "lens")
-    _lengths(sel_table, B * Hkv * keep, "sel_table")
-    _lengths(sel_len, B * Hkv, "sel_len")
-    _called("paged_select", cache._dev, *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, d, lens.data_ptr(), int(keep), int(n_first),
-            int(n_last), sel_table.data_ptr(), sel_len.data_ptr(), _ptr(status), _stream(q))
+    _lengths(lens, B * cache.table_heads, dev, "lens")
+    _lengths(sel_table, B * Hkv * keep, dev, "sel_table")
+    _lengths(sel_len, B * Hkv, dev, "sel_len")
+    code = _called(_native().paged_select, dev, (
+        *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, cache.d, lens.data_ptr(), int(keep), int(n_first), int(n_last),
+        sel_table.data_ptr(), sel_len.data_ptr(), _ptr(status), _stream(q)))
+    if code != SC_OK:
+        raise ScError("sc_paged_select", code)
 
 
 def paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, *, seq_len=None, count_new=None, inv_freq=None, positions=None,
@@ -748,7 +758,7 @@ def paged_decode_attn(q, cache: PagedCache, lens, out=None, workspace=None, scal
         out = torch.empty_like(q)
     if workspace is None:
         B, Hq, d = q.shape
-        workspace = paged_decode_workspace(B, Hq, cache.heads if cache.heads > 1 else cache.table_heads, d, q.device)
+        workspace = paged_decode_workspace(B, Hq, cache.Hkv, d, q.device)
     sc_paged_decode_attn(q, cache, lens, out, workspace, scale, status, flags)
     return out
 
@@ -756,8 +766,7 @@ def paged_decode_attn(q, cache: PagedCache, lens, out=None, workspace=None, scal
 def paged_select(q, cache: PagedCache, lens, keep: int, n_first: int = 0, n_last: int = 1, status=None):
     """Picks pages for sparse attention.  Returns (table [B, Hkv, keep], lengths [B, Hkv]) for
     ``paged_decode_attn(q, cache.over(table), lengths)``."""
-    Hkv = cache.heads if cache.heads > 1 else cache.table_heads
-    table = torch.empty((cache.B, Hkv, keep), dtype=torch.int32, device=q.device)
-    lengths = torch.empty((cache.B, Hkv), dtype=torch.int32, device=q.device)
+    table = torch.empty((cache.B, cache.Hkv, keep), dtype=torch.int32, device=q.device)
+    lengths = torch.empty((cache.B, cache.Hkv), dtype=torch.int32, device=q.device)
     sc_paged_select(q, cache, lens, keep, n_first, n_last, table, lengths, status)
     return table, lengths

@@ -2,10 +2,10 @@
 //
 // One block serves one piece of one sequence: the new rows that fall into one page, for some of the heads (keys, values and
 // queries counted in one row).  So a page's bounds belong to one block per head, whose warps hold whole heads: smallest and
-// largest key are taken in registers over the piece's rows and meet in a few shuffles; no atomics.  The host knows T and B only:
-// block x serves the sequence b with f(b) <= x < f(b + 1), f(b) = seq_off[b] / page_size + 2 b, and its piece x - f(b); n rows
-// touch at most n / page_size + 2 pages, so every piece has a block, and every block finds its sequence with one look at the
-// offsets.  Sines and cosines of a piece's rows are taken once per block, 16 rows at a time, and shared by its heads.
+// largest key are taken in registers over the piece's rows and meet in a few shuffles; no atomics.  The host knows T and B only, from which
+// follow the most pieces there can be; which piece is a block's own it finds by counting all sequences' pieces.  (Places for two pieces more than
+// n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us.)
+// Sines and cosines of a piece's rows are taken once per block, 16 rows at a time, and shared by its heads.
 #include "paged.cuh"
 
 namespace sc {
@@ -58,55 +58,71 @@ template <typename T> struct Vec<T, 1> {
 __device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
 __device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
-// cos and sin of position * freq.  The product of an int32 and a float is exact in 64 bits; in turns (times 1 / 2 pi) its whole part is dropped
-// there too, and what is left, at most half a turn, is exact enough in 32 bits whatever the position was.
-__device__ __forceinline__ float2 turn(int position, float freq) {
-    double t = (double)position * (double)freq * 0.15915494309189533577;
-    t -= rint(t);
+// Angles are taken in turns as 64-bit fixed-point fractions, whose wrap-around is the whole turns': the step of a pair, freq / 2 pi, once per block
+// and pair in two doubles (1 / 2 pi = kTurn + kTurnRest to 107 bits), then one integer product per position, off by 2^-34 of a turn at
+// the farthest position.  (In doubles per position and pair it was a quarter of all instructions of a long prompt.)
+constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;
+__device__ __forceinline__ uint64_t turn_step(float freq) {
+    const double f = freq, hi = f * kTurn, lo = fma(f, kTurn, -hi) + f * kTurnRest;
+    const double part = hi - rint(hi);                      // exact, in [-1/2, 1/2]
+    return (uint64_t)(int64_t)rint(part * 0x1p62) * 4 + (uint64_t)(int64_t)rint(lo * 0x1p64);   // (2^62: 2^63 is no int64)
+}
+__device__ __forceinline__ float2 turn(int position, uint64_t step) {
+    const int32_t t = (int32_t)(((uint64_t)(int64_t)position * step) >> 32);   // in 2^-32 turns
     float s, c;
-    sincospif((float)(2.0 * t), &s, &c);
+    sincospif((float)t * 0x1p-31f, &s, &c);
     return make_float2(c, s);
 }
 
 struct Dims { int B, Hq, Hkv, T, d, group; };
 
-template <typename T, int E, bool kPairs>
-__global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, const sc_paged_rows rows, const Dims dims, int32_t* status) {
-    __shared__ float2 sh_cs[kSub * kMaxHalf];
-    __shared__ int sh_seq;
+// E: elements of a vector.  kUnits: units of a row (see below) where they fill a power of two of lanes and all columns are rotated, or none; 0: any.
+template <typename T, int E, bool kPairs, int kUnits>
+__global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages, const sc_paged_rows rows, const Dims dims, int32_t* status) {
+    // Cosines and sines of a row, in the order in which lanes take them: lane u the pairs u * E .. u * E + E - 1, four at a time, so that
+    // each four of neighbouring lanes lie side by side (as a plain list of pairs, read with 16-way bank conflicts, 35 K tokens x 48 heads took 265 us).
+    __shared__ __align__(16) float sh_cos[kSub * kMaxHalf], sh_sin[kSub * kMaxHalf];
+    __shared__ uint64_t sh_step[kMaxHalf];
+    __shared__ int sh_seq, sh_piece, sh_sums[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = pages.page_size, B = dims.B, Hkv = dims.Hkv, d = dims.d;
     if (tid == 0) sh_seq = -1;
     in_stream_order();
     __syncthreads();
-    for (int b = tid; b < B; b += kThreads) {
-        const int o0 = rows.seq_off[b], o1 = rows.seq_off[b + 1];
-        if (o0 < 0 || o1 < o0 || o1 > dims.T) {
-            if (blockIdx.x == 0 && blockIdx.y == 0) set_status(status, SC_ERR_INVALID_ARG);
-            continue;
+    const int rot = rows.inv_freq != nullptr ? rows.rot_dim : 0, half = rot / 2;
+    for (int i = tid; i < half; i += kThreads) sh_step[i] = turn_step(rows.inv_freq[i]);
+    int before = 0;                              // pieces of the sequences before these 256
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        const int b = b0 + tid;
+        int pieces = 0;
+        if (b < B) {
+            const int o0 = rows.seq_off[b], o1 = rows.seq_off[b + 1], have = rows.cache_len[b];
+            const int n = rows.seq_len != nullptr ? rows.seq_len[b] : o1 - o0;
+            const bool placed = o0 >= 0 && o1 >= o0 && o1 <= dims.T, valid = placed && n >= 0 && n <= o1 - o0 && have >= 0;
+            const bool fits = valid && (int64_t)have + n <= pages.cap();
+            if (valid && n > 0) pieces = (have % ps + n - 1) / ps + 1;
+            if (blockIdx.y == 0 && b % gridDim.x == blockIdx.x) {
+                if (!fits) set_status(status, valid ? SC_ERR_CAPACITY : SC_ERR_INVALID_ARG);
+                if (rows.len_out != nullptr) rows.len_out[b] = fits ? have + n : have;
+            }
         }
-        const int64_t f0 = o0 / ps + 2ll * b, f1 = o1 / ps + 2ll * (b + 1);
-        if (f0 <= blockIdx.x && blockIdx.x < f1) sh_seq = b;   // (offsets that do not fall: one sequence at most)
+        const int upto = warp_scan_add(pieces, lane);
+        if (lane == 31) sh_sums[warp] = upto;
+        __syncthreads();
+        int first = before + upto - pieces;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            first += w < warp ? sh_sums[w] : 0;
+            before += sh_sums[w];
+        }
+        if ((unsigned)((int)blockIdx.x - first) < (unsigned)pieces) { sh_seq = b; sh_piece = (int)blockIdx.x - first; }
+        __syncthreads();
     }
-    __syncthreads();
-    const int b = sh_seq;
+    const int b = sh_seq, piece = sh_piece;
     if (b < 0) return;
-    const int o0 = rows.seq_off[b], range = rows.seq_off[b + 1] - o0;
-    const int piece = (int)(blockIdx.x - (o0 / ps + 2ll * b));
-    const int n = rows.seq_len != nullptr ? rows.seq_len[b] : range;
-    const int have = rows.cache_len[b];
-    if (n < 0 || n > range || have < 0) {
-        if (piece == 0 && blockIdx.y == 0 && tid == 0) {
-            set_status(status, SC_ERR_INVALID_ARG);
-            if (rows.len_out != nullptr) rows.len_out[b] = have;
-        }
-        return;
-    }
+    const int o0 = rows.seq_off[b], have = rows.cache_len[b];
+    const int n = rows.seq_len != nullptr ? rows.seq_len[b] : rows.seq_off[b + 1] - o0;
     const bool fits = (int64_t)have + n <= pages.cap();
-    if (piece == 0 && blockIdx.y == 0 && tid == 0) {
-        if (!fits) set_status(status, SC_ERR_CAPACITY);
-        if (rows.len_out != nullptr) rows.len_out[b] = fits ? have + n : have;
-    }
     // the piece: rows [r0, r1) of the sequence (64 bits: a length near 2^31 with rows that do not fit)
     const int64_t slot = have / ps + (int64_t)piece, p0 = slot * ps;
     const int64_t r0 = p0 > have ? p0 : have, r1 = min(p0 + ps, (int64_t)have + n);
@@ -120,7 +136,6 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
             if (blockIdx.y == 0 && tid == 0) set_status(status, SC_ERR_INVALID_ARG);
         }
     }
-    const int rot = rows.inv_freq != nullptr ? rows.rot_dim : 0, half = rot / 2;
     const int heads = 2 * Hkv + (rows.q != nullptr ? dims.Hq : 0);
     int h_lo = blockIdx.y * dims.group;
     const int h_hi = min(h_lo + dims.group, heads);
@@ -128,15 +143,18 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
     if (h_lo >= h_hi) return;
 
     // A row is d / E vectors, taken two at a time: a unit is the two that rotate into each other (or two neighbours).
-    const int n_vec = d / E, rot_units = kPairs ? 0 : half / E;
-    const int units = rot_units + (n_vec - 2 * rot_units + 1) / 2;
-    int unit_lanes = 1;
-    while (unit_lanes < units && unit_lanes < 32) unit_lanes *= 2;
+    const int n_vec = kUnits ? 2 * kUnits : d / E, rot_units = kUnits ? (kPairs || half == 0 ? 0 : kUnits) : kPairs ? 0 : half / E;
+    const int units = kUnits ? kUnits : rot_units + (n_vec - 2 * rot_units + 1) / 2;
+    int unit_lanes = kUnits ? kUnits : 1;
+    while (!kUnits && unit_lanes < units && unit_lanes < 32) unit_lanes *= 2;
     const int slots = 32 / unit_lanes;      // rows, or rows of several heads, a warp holds at once
     int row_slots = 1;
     while (row_slots < nr && row_slots < slots) row_slots *= 2;
     const int head_slots = slots / row_slots;
     const int lu = lane % unit_lanes, lr = lane / unit_lanes % row_slots, lh = lane / (unit_lanes * row_slots);
+    constexpr int kFour = E < 4 ? 1 : 4;
+    const int turned_units = (half + E - 1) / E, cs_row = turned_units * E;
+    const auto place_of_pair = [&](int c) { return (c % E / kFour * turned_units + c / E) * kFour + c % kFour; };
     const int64_t page_at = (int64_t)id * pages.page_stride;
     const bool bounds = pages.k_min != nullptr && id >= 0;
 
@@ -146,7 +164,9 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
         for (int i = tid; i < ns * half; i += kThreads) {
             const int r = i / half, c = i - r * half;
             const int pos = rows.positions != nullptr ? rows.positions[tok0 + s0 + r] : (int)(r0 + s0 + r);
-            sh_cs[i] = turn(pos, rows.inv_freq[c]);
+            const float2 t = turn(pos, sh_step[c]);
+            sh_cos[r * cs_row + place_of_pair(c)] = t.x;
+            sh_sin[r * cs_row + place_of_pair(c)] = t.y;
         }
         if (pages.count != nullptr && blockIdx.y == 0 && id >= 0)
             for (int i = tid; i < ns * Hkv; i += kThreads) {
@@ -173,19 +193,30 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
             }
             for (int u0 = 0; u0 < units; u0 += unit_lanes) {
                 const int u = u0 + lu;
-                const bool turned = !is_v && (kPairs ? 2 * u * E < rot : u < rot_units);
+                const bool turned = !is_v && (kUnits ? half > 0 : kPairs ? 2 * u * E < rot : u < rot_units);
                 const int va = u < rot_units ? u : 2 * rot_units + 2 * (u - rot_units), vb = u < rot_units ? u + rot_units : va + 1;
-                const bool has_a = active && u < units, has_b = has_a && vb < n_vec;
+                const bool has_a = active && (kUnits || u < units), has_b = kUnits ? has_a : has_a && vb < n_vec;
                 float lo_a[E], hi_a[E], lo_b[E], hi_b[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) { lo_a[e] = lo_b[e] = INFINITY; hi_a[e] = hi_b[e] = -INFINITY; }
+                // a page whose first row is new starts afresh; of another one the bounds so far are requested beside the rows (the same thread
+                // comes back here with the next rows of a longer piece)
+                const bool mine = bounds && is_k && has_a && lr == 0, widen = mine && in_page + s0 > 0;
+                T* mn = pages.k_min + ((int64_t)id * pages.page_heads + x) * d;
+                T* mx = pages.k_max + ((int64_t)id * pages.page_heads + x) * d;
+                Vec<T, E> old[4];
+                if (widen) {
+                    old[0].load(mn + va * E); old[1].load(mx + va * E);
+                    if (has_b) { old[2].load(mn + vb * E); old[3].load(mx + vb * E); }
+                }
                 for (int rb = lr; rb < ns; rb += 4 * row_slots) {   // four rows requested together
                     Vec<T, E> a[4], c[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int r = rb + j * row_slots;
-                        if (r < ns && has_a) a[j].load(src + r * src_row + va * E);
-                        if (r < ns && has_b) c[j].load(src + r * src_row + vb * E);
+                        const T* at = src + r * src_row;
+                        if (r < ns && has_a) a[j].load(at + va * E);
+                        if (r < ns && has_b) c[j].load(at + vb * E);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -195,35 +226,40 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
                             float xa[E], xb[E];
                             a[j].get(xa);
                             if (has_b) c[j].get(xb);
-                            const float2* cs = sh_cs + r * half;
-                            if constexpr (kPairs) {
+                            float cosv[E], sinv[E];
 #pragma unroll
-                                for (int e = 0; e < E; e += 2) {
-                                    const int pa = (va * E + e) / 2, pb = (vb * E + e) / 2;
-                                    if (pa < half) {
-                                        const float2 t = cs[pa];
-                                        const float y1 = xa[e] * t.x - xa[e + 1] * t.y, y2 = xa[e + 1] * t.x + xa[e] * t.y;
-                                        xa[e] = y1; xa[e + 1] = y2;
-                                    }
-                                    if (has_b && pb < half) {
-                                        const float2 t = cs[pb];
-                                        const float y1 = xb[e] * t.x - xb[e + 1] * t.y, y2 = xb[e + 1] * t.x + xb[e] * t.y;
-                                        xb[e] = y1; xb[e + 1] = y2;
-                                    }
+                            for (int f = 0; f < E / kFour; ++f) {
+                                const int at = r * cs_row + (f * turned_units + u) * kFour;
+                                if constexpr (kFour == 4) {
+                                    const float4 x4 = *reinterpret_cast<const float4*>(sh_cos + at), y4 = *reinterpret_cast<const float4*>(sh_sin + at);
+                                    cosv[4 * f] = x4.x; cosv[4 * f + 1] = x4.y; cosv[4 * f + 2] = x4.z; cosv[4 * f + 3] = x4.w;
+                                    sinv[4 * f] = y4.x; sinv[4 * f + 1] = y4.y; sinv[4 * f + 2] = y4.z; sinv[4 * f + 3] = y4.w;
+                                } else {
+                                    cosv[f] = sh_cos[at]; sinv[f] = sh_sin[at];
+                                }
+                            }
+                            if constexpr (kPairs) {   // (columns 2 u E on: pairs u E on)
+#pragma unroll
+                                for (int e = 0; e < E; ++e) {
+                                    if (!kUnits && u * E + e >= half) break;
+                                    float& x1 = e < E / 2 ? xa[2 * e] : xb[2 * e - E];
+                                    float& x2 = e < E / 2 ? xa[2 * e + 1] : xb[2 * e - E + 1];
+                                    const float y1 = x1 * cosv[e] - x2 * sinv[e], y2 = x2 * cosv[e] + x1 * sinv[e];
+                                    x1 = y1; x2 = y2;
                                 }
                             } else {
 #pragma unroll
                                 for (int e = 0; e < E; ++e) {
-                                    const float2 t = cs[u * E + e];
-                                    const float y1 = xa[e] * t.x - xb[e] * t.y, y2 = xb[e] * t.x + xa[e] * t.y;
+                                    const float y1 = xa[e] * cosv[e] - xb[e] * sinv[e], y2 = xb[e] * cosv[e] + xa[e] * sinv[e];
                                     xa[e] = y1; xb[e] = y2;
                                 }
                             }
                             a[j].set(xa);
                             if (has_b) c[j].set(xb);
                         }
-                        a[j].store(dst + r * dst_row + va * E);
-                        if (has_b) c[j].store(dst + r * dst_row + vb * E);
+                        T* to = dst + r * dst_row;
+                        a[j].store(to + va * E);
+                        if (has_b) c[j].store(to + vb * E);
                         if (bounds && is_k) {   // of what is stored
                             float xa[E], xb[E];
                             a[j].get(xa);
@@ -245,26 +281,21 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
                         lo_b[e] = min_nan(lo_b[e], __shfl_xor_sync(kFull, lo_b[e], o)); hi_b[e] = max_nan(hi_b[e], __shfl_xor_sync(kFull, hi_b[e], o));
                     }
                 }
-                if (is_k && has_a && lr == 0) {
-                    // a page whose first row is new starts afresh; the same thread comes back here with the next rows of a longer piece
-                    const bool widen = in_page + s0 > 0;
-                    T* mn = pages.k_min + ((int64_t)id * pages.page_heads + x) * d;
-                    T* mx = pages.k_max + ((int64_t)id * pages.page_heads + x) * d;
-                    const auto put = [&](T* at, float (&v)[E], bool smaller) {
+                if (mine) {
+                    const auto put = [&](T* at, float (&v)[E], const Vec<T, E>& was, bool smaller) {
                         Vec<T, E> w;
                         if (widen) {
-                            float old[E];
-                            w.load(at);
-                            w.get(old);
+                            float o[E];
+                            was.get(o);
 #pragma unroll
-                            for (int e = 0; e < E; ++e) v[e] = smaller ? min_nan(v[e], old[e]) : max_nan(v[e], old[e]);
+                            for (int e = 0; e < E; ++e) v[e] = smaller ? min_nan(v[e], o[e]) : max_nan(v[e], o[e]);
                         }
                         w.set(v);
                         w.store(at);
                     };
-                    put(mn + va * E, lo_a, true);
-                    put(mx + va * E, hi_a, false);
-                    if (has_b) { put(mn + vb * E, lo_b, true); put(mx + vb * E, hi_b, false); }
+                    put(mn + va * E, lo_a, old[0], true);
+                    put(mx + va * E, hi_a, old[1], false);
+                    if (has_b) { put(mn + vb * E, lo_b, old[2], true); put(mx + vb * E, hi_b, old[3], false); }
                 }
             }
         }
@@ -274,17 +305,32 @@ __global__ void __launch_bounds__(kThreads) append_paged(const Pages<T> pages, c
 template <typename T, int E>
 cudaError_t run(const PagedAppendArgs& a, cudaStream_t st) {
     const int heads = 2 * a.Hkv + (a.rows.q != nullptr ? a.Hq : 0);
-    const int groups = div_up(heads, kGroupHeads);
+    // heads per block: 32, or down to 8 where that leaves SMs idle
+    int dev = 0, sms = 148;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    int64_t blocks = a.T / a.cache.page_size + 2ll * a.B;   // n rows touch n / page_size + 2 pages at most, and no more than n
+    if (blocks > a.T) blocks = a.T > 0 ? a.T : 1;
+    const int64_t pieces = blocks < a.T / a.cache.page_size + a.B ? blocks : a.T / a.cache.page_size + a.B;   // about
+    int64_t groups = div_up(heads, kGroupHeads);
+    if (groups * pieces < 2 * sms) groups = 2 * sms / pieces < div_up(heads, 8) ? 2 * sms / pieces : div_up(heads, 8);
     const Dims dims = {a.B, a.Hq, a.Hkv, a.T, a.d, div_up(heads, groups)};
-    const int64_t blocks = a.T / a.cache.page_size + 2ll * a.B;
     if (blocks > 0x7fffffff || groups > 65535) return cudaErrorInvalidConfiguration;
     const Pages<T> pages = pages_of<T>(a.cache);
-    const dim3 grid((unsigned)blocks, groups);
+    const dim3 grid((unsigned)blocks, (unsigned)groups);
     const bool pairs = (a.flags & SC_FLAG_ROPE_PAIRS) != 0;
-    // Two halves that are not whole vectors are rotated element by element.
-    if (!pairs && a.rows.inv_freq != nullptr && (a.rows.rot_dim / 2) % E != 0)
-        return launch_in_order(append_paged<T, 1, false>, grid, kThreads, 0, st, pages, a.rows, dims, a.status);
-    return launch_in_order(pairs ? append_paged<T, E, true> : append_paged<T, E, false>, grid, kThreads, 0, st, pages, a.rows, dims, a.status);
+    const int rot = a.rows.inv_freq != nullptr ? a.rows.rot_dim : 0, units = a.d % (2 * E) == 0 && (rot == 0 || rot == a.d) ? a.d / (2 * E) : 0;
+    const auto kernel = [&] {
+        // Two halves that are not whole vectors are rotated element by element.
+        if (!pairs && (rot / 2) % E != 0) return append_paged<T, 1, false, 0>;
+        switch (units) {
+            case 4: return pairs ? append_paged<T, E, true, 4> : append_paged<T, E, false, 4>;
+            case 8: return pairs ? append_paged<T, E, true, 8> : append_paged<T, E, false, 8>;
+            case 16: return pairs ? append_paged<T, E, true, 16> : append_paged<T, E, false, 16>;
+            default: return pairs ? append_paged<T, E, true, 0> : append_paged<T, E, false, 0>;
+        }
+    }();
+    return launch_in_order(kernel, grid, kThreads, 0, st, pages, a.rows, dims, a.status);
 }
 
 }  // namespace
