@@ -71,8 +71,7 @@ sc_status sc_paged_append(const sc_paged_cache* cache, const sc_paged_rows* rows
 
 size_t sc_paged_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0) return 256;
-    const size_t a = paged_decode_generic_ws_bytes(d < 256 ? d : 256), b = paged_decode_mma_ws_bytes();
-    return a > b ? a : b;
+    return paged_decode_ws_bytes();
 }
 
 sc_status sc_paged_decode_attn(const sc_paged_cache* cache, const void* q, sc_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,

@@ -11,31 +11,18 @@
 // Up to four query heads stand in the eight columns twice, the second time for the remainders.  Warps meet in shared memory, blocks of a
 // cluster hand each other slices of their sums through distributed shared memory (decode_fold.cuh), parties that share a unit leave
 // partial sums in global memory, slice by slice, and the last to arrive joins them.  Every order is fixed: results are bit-reproducible.
-#include <cooperative_groups.h>
-
 #include <mutex>
 
-#include "decode_fold.cuh"
-#include "paged.cuh"
+#include "paged_attn.cuh"
 
 namespace sc {
 namespace pg {
 
 namespace {
 
-namespace cg = cooperative_groups;
-
 typedef __nv_bfloat16 bf16;
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-constexpr int kTile = 16;
-constexpr int kHeads = 8;                 // query heads at a time
 constexpr float kMaxSlack = 8.f;          // log2 units a score may exceed the running maximum before it is raised
-constexpr int kMaxBlocks = 320;           // of a launch
-constexpr int kMergeGroup = 8;            // partial sums read together
-constexpr unsigned kShortStretch = 64;    // tiles per block below which stretches are cut at the units' ends
-constexpr int kLeastShared = 2, kLeastAlone = 2;   // tiles per warp that a stretch of a cluster, or of a block, has at least
 
 template <int D>
 struct Shape {
@@ -45,24 +32,11 @@ struct Shape {
     static constexpr int kTileBytes = kTile * kRowBytes;             // of K or V
     static constexpr int kStageBytes = 2 * kTileBytes + 80;          // K, V, 16 counts, which rows count
     static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
-    static constexpr int kRecvO = (kHeads * (D / 4) + dm::kMaxCluster) * 16;   // slices of O from a cluster's blocks, rounded up
-    static constexpr int kRecvBytes = kRecvO + dm::kMaxCluster * kHeads * 8;   // and m, l
-    static constexpr int kSmemBytes = kRingBytes + 2 * kRecvBytes;
-    static constexpr int kPartStride = kHeads * D + 2 * kHeads;      // floats: acc[8][D], m[8], l[8]
+    static constexpr int kSmemBytes = kRingBytes + 2 * recv_bytes(D, kHeads);
     static_assert(kWarps * kHeads * D * 4 <= kRingBytes, "the warps' sums lie in the ring's place");
 };
 static_assert(kMaxBlocks * 4 <= (int)kTicketBytes, "a counter per party and slice");
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int src_bytes) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
@@ -89,43 +63,17 @@ __device__ __forceinline__ float fast_log2(float x) {
     asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void store_out4(bf16* dst, const float4& o, float l) {   // (no row: zeros; l not a number: not a number)
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    const uint2 w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    *reinterpret_cast<uint2*>(dst) = w;
-}
-
 // One head's rows as a warp copies them: tile after tile into stages.
 template <int D, bool kWhole>
 struct Rows {
     const bf16* k; const bf16* v;      // of the head inside the pages
     const int32_t* count;              // likewise, or NULL
-    const int32_t* table;
     const void* nowhere;               // a valid address for copies of no bytes
     int64_t page_stride, row_stride;
     int64_t count_page;
-    int num_pages, page_size, len;
+    int num_pages, len;
     int32_t* status;
 
-    // Pages are looked up for kBatch of the warp's tiles at a time (its j-th is tile first + j * kWarps), a batch ahead: one load, whose latency
-    // is longer than a tile takes.  kWhole (page_size a multiple of 16: a tile lies in one page): lane l has the batch's l-th tile; else the
-    // row lane & 15 of its (l / 16)-th.  x: the page, -1: no such row;  y: the row's (the tile's first row's) place in it.
-    static constexpr int kBatch = kWhole ? 32 : 2;
-    __device__ __forceinline__ int2 look_up(int first, int j0, int n, int lane) const {
-        const int j = j0 + (kWhole ? lane : lane >> 4);
-        int2 at = make_int2(-1, 0);
-        if (j >= n) return at;
-        const int row = (first + j * kWarps) * kTile + (kWhole ? 0 : lane & 15);
-        if (row < len) {
-            const int slot = row / page_size;
-            at = make_int2(table[slot], row - slot * page_size);
-        }
-        return at;
-    }
-    __device__ __forceinline__ int2 of_batch(const int2& batch, int j, int lane) const {
-        const int src = kWhole ? j & 31 : (j & 1) * 16 + (lane & 15);
-        return make_int2(__shfl_sync(kFull, batch.x, src), __shfl_sync(kFull, batch.y, src));
-    }
     __device__ __forceinline__ void copy(uint32_t stage, int tile, int2 at, int lane) const {
         constexpr int kChunks = D / 8, kStep = 32 / kChunks, kN = kTile / kStep;   // lanes per row, rows per round, rounds
         using S = Shape<D>;
@@ -190,62 +138,16 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
     __shared__ __align__(8) unsigned long long sh_bar[2];   // what the cluster's blocks hand this one, segments by turns
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, tig = lane & 3;
-    int csize = (int)cg::this_cluster().num_blocks(), crank = (int)cg::this_cluster().block_rank(), party = blockIdx.x / csize;
-    if (csize > 1) {
-        if (threadIdx.x == 0) {
-            umma::mbar_init(smem_u32(&sh_bar[0]), 1);
-            umma::mbar_init(smem_u32(&sh_bar[1]), 1);
-            umma::mbar_fence_init();
-        }
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // (waited for before the first hand-over)
-    }
+    Party me;
+    me.set_up(sh_bar);
     in_stream_order();
-
-    const int G = Hq / Hkv, groups = (G + kHeads - 1) / kHeads;
-    const auto head_of = [&](int entry, int unit, int& b, int& h, int& g0) {
-        b = entry / pages.table_heads;
-        h = pages.table_heads > 1 ? entry - b * pages.table_heads : unit / groups;
-        g0 = unit % groups * kHeads;
-    };
-    const auto zero_empty = [&] {   // heads without rows
-        for (int e = blockIdx.x; e < line.entries; e += gridDim.x) {
-            if (line.len(e) > 0) continue;
-            for (int i = threadIdx.x; i < line.per_entry * kHeads * (D / 4); i += kThreads) {
-                int b, h, g0;
-                const int g1 = i / (D / 4) % kHeads;
-                head_of(e, i / (kHeads * (D / 4)), b, h, g0);
-                if (g0 + g1 < G) store_out4(out + ((int64_t)b * Hq + h * G + g0 + g1) * D + i % (D / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
-            }
-        }
-    };
-    unsigned total = total_of(line, lane);
-    bool in_step = csize == 1;   // the cluster's blocks are known to have started
-    if (total < short_below) {   // each block for itself (see start())
-        if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-        in_step = true;
-        csize = 1; crank = 0; party = blockIdx.x;
-        line.parties = gridDim.x;
-    }
-    const unsigned least = csize * kWarps * (csize > 1 ? kLeastShared : kLeastAlone);
-    const unsigned stretch = max((total + line.parties - 1) / line.parties, least);
-    const bool cut = stretch < kShortStretch * csize && line.entries <= 64 && line.entries * line.per_entry <= line.parties;   // at the units' ends
-    Part own = {0, 0, 0, 0, 0, 0};
-    unsigned from = 0, left;
-    if (cut) {
-        own = part_of(line, stretch, party, lane);
-        left = own.take;
-    } else {
-        from = min((uint64_t)party * stretch, (uint64_t)total);
-        left = min(stretch, total - from);
-    }
-    if (left == 0) {
-        zero_empty();
-        if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    const int G = Hq / Hkv;
+    if (!me.plan(line, short_below, lane)) {
+        zero_empty(pages, line, Hq, G, kHeads, D, out);
+        me.step();
         return;
     }
-    bool got = true;             // no wait has given up
-    unsigned turn = 0;           // of the segment: which barrier, and its phase
+    Joiner joiner = {sh_bar, smem + S::kRingBytes, &sh_last, tickets, part, status, kHeads, 0u, true};
 
     // per-lane ldmatrix row/chunk selectors
     const int lm_j = lane >> 3, lm_r = lane & 7;
@@ -253,34 +155,28 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
     const int v_row = lm_r + ((lm_j >> 1) << 3), v_csel = lm_j & 1;    // V^T: (r0-7,c), (r0-7,c+1), (r8-15,c), (r8-15,c+1)
     const uint32_t ring = smem_u32(smem) + warp * (S::kStages * S::kStageBytes);
 
-    for (Place p = cut ? Place{own.entry, own.unit, own.tile, 0u} : place_of(line, from, lane);;) {
+    for (Place p = me.begin(line, lane);;) {
         const int len = line.len(p.entry), nt = line.tiles(p.entry);
-        const int take = (int)min((unsigned)(nt - p.tile), left);
-        int b, h, g0;
-        head_of(p.entry, p.unit, b, h, g0);
-        const int nh = min(kHeads, G - g0);
-        const int64_t hq0 = (int64_t)b * Hq + h * G + g0;
+        const int take = (int)min((unsigned)(nt - p.tile), me.left);
+        const Unit unit(pages, p.entry, p.unit, G, kHeads);
+        const int nh = unit.nh;
+        const int64_t hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
         // this block's tiles of the segment, and this warp's: t0 + warp, t0 + warp + kWarps, ...
-        const int each = (take + csize - 1) / csize, t0 = p.tile + min(crank * each, take), t1 = p.tile + min((crank + 1) * each, take);
+        const int each = (take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, take), t1 = p.tile + min((me.crank + 1) * each, take);
         const int my_tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
         Rows<D, kWhole> rows;
         {
-            const int hp = pages.page_heads > 1 ? h : 0;
+            const int hp = pages.page_heads > 1 ? unit.h : 0;
             rows.k = pages.k + hp * pages.head_stride; rows.v = pages.v + hp * pages.head_stride;
             rows.count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
             rows.count_page = (int64_t)pages.page_heads * pages.page_size;
-            rows.table = pages.table_of(p.entry); rows.nowhere = q;
+            rows.nowhere = q;
             rows.page_stride = pages.page_stride; rows.row_stride = pages.row_stride;
-            rows.num_pages = pages.num_pages; rows.page_size = pages.page_size; rows.len = len; rows.status = status;
+            rows.num_pages = pages.num_pages; rows.len = len; rows.status = status;
         }
-        int2 batch = rows.look_up(t0 + warp, 0, my_tiles, lane), next_batch = rows.look_up(t0 + warp, rows.kBatch, my_tiles, lane);
-        const auto copy = [&](uint32_t stage, int j) {   // the warp's j-th tile, j = 0, 1, ...
-            if (j % rows.kBatch == 0 && j > 0) {
-                batch = next_batch;
-                next_batch = rows.look_up(t0 + warp, j + rows.kBatch, my_tiles, lane);
-            }
-            rows.copy(stage, t0 + warp + j * kWarps, rows.of_batch(batch, j, lane), lane);
-        };
+        Finder<kWhole> finder = {pages.table_of(p.entry), pages.page_size, len, t0 + warp, my_tiles, {}, {}};
+        finder.start(lane);
+        const auto copy = [&](uint32_t stage, int j) { rows.copy(stage, t0 + warp + j * kWarps, finder.get(j, lane), lane); };   // the warp's j-th tile
 #pragma unroll
         for (int s = 0; s < S::kStages; ++s) {
             if (s < my_tiles) copy(ring + s * S::kStageBytes, s);
@@ -422,111 +318,14 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             for (int w = 0; w < kWarps; ++w) bl += sh_m[w][hd] == -INFINITY ? 0.f : sh_l[w][hd] * dm::fast_exp2(sh_m[w][hd] - bm);
             return make_float2(bm, bl);
         };
-        const bool whole = take == nt;
-        const int n4 = nh * (D / 4), slice = (n4 + csize - 1) / csize, e_lo = min(crank * slice, n4), e_hi = min(e_lo + slice, n4);
-        float* mine = part + (size_t)(2 * party + (!cut && p.at > from)) * S::kPartStride;
-        const auto give = [&](int e4, const float4& acc, float m, float l) {
-            const int hd = e4 / (D / 4), d4 = e4 % (D / 4) * 4;
-            if (whole) {
-                store_out4(out + (hq0 + hd) * D + d4, acc, l);
-            } else {
-                *reinterpret_cast<float4*>(mine + hd * D + d4) = acc;
-                if (d4 == 0 || e4 == e_lo) { mine[kHeads * D + hd] = m; mine[kHeads * D + kHeads + hd] = l; }   // (the same from every slice of the head)
-            }
-        };
-        if (csize == 1) {
-            for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
-                const float2 ml = block_ml(e4 / (D / 4));
-                give(e4, block_sum(e4), ml.x, ml.y);
-            }
-        } else {
-            // Every block hands slice r of its sums to block r, which folds it.  A block's receiving places are used by turns: who hands it
-            // something for the segment after the next has its slice of the next one, so it is done with this one.
-            const uint32_t bar = smem_u32(&sh_bar[turn & 1]);
-            unsigned char* recv = smem + S::kRingBytes + (turn & 1) * S::kRecvBytes;
-            float4* recv_o = reinterpret_cast<float4*>(recv);
-            float* recv_ml = reinterpret_cast<float*>(recv + S::kRecvO);
-            if (threadIdx.x == 0) umma::mbar_expect_tx(bar, (uint32_t)(csize * ((e_hi - e_lo) * 16 + kHeads * 8)));
-            if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // every block of the cluster has started
-            in_step = true;
-            for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
-                const int to = e4 / slice;
-                dm::hand_over(dm::mapa(smem_u32(recv_o + crank * slice + (e4 - to * slice)), to), dm::mapa(bar, to), block_sum(e4));
-            }
-            for (int x = threadIdx.x; x < csize * kHeads; x += kThreads) {
-                const float2 ml = block_ml(x & 7);
-                dm::hand_over(dm::mapa(smem_u32(recv_ml + crank * 2 * kHeads + (x & 7) * 2), x >> 3), dm::mapa(bar, x >> 3), ml.x, ml.y);
-            }
-            if (got) got = umma::mbar_wait<true>(bar, turn >> 1 & 1);
-            if (!got) set_status(status, SC_ERR_TIMEOUT);
-            for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
-                const dm::Folded f = dm::fold_slices(recv_o, recv_ml, csize, slice, e4 - e_lo, e4 / (D / 4), got);
-                give(e4, f.o, f.m, f.l);
-            }
-            ++turn;
-        }
-        if (!whole) {
-            // Parties that share a unit: the last one to bring a slice joins the slice's parts in order.
-            const unsigned first = cut ? party - own.index : p.at / stretch, last = cut ? first + own.parts - 1 : (p.at + nt - 1) / stretch;
-            int32_t* ticket = tickets + (first * csize + crank);   // (a party begins one shared unit at most)
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int t;
-                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(t) : "l"(ticket) : "memory");
-                sh_last = t == (int)(last - first);
-                if (sh_last) *ticket = 0;   // ready for the next call
-            }
-            __syncthreads();
-            if (sh_last) {
-                for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
-                    const int hd = e4 / (D / 4), d4 = e4 % (D / 4) * 4;
-                    float m = -INFINITY, l = 0.f;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (unsigned j0 = first; j0 <= last; j0 += kMergeGroup) {
-                        float mv[kMergeGroup], lv[kMergeGroup];
-                        float4 ov[kMergeGroup];
-#pragma unroll
-                        for (int j = 0; j < kMergeGroup; ++j) {
-                            const bool ok = j0 + j <= last;
-                            const unsigned w = ok ? j0 + j : first;
-                            const float* sp = part + (size_t)(2 * w + (!cut && p.at > w * stretch)) * S::kPartStride;
-                            mv[j] = ok ? __ldcg(sp + kHeads * D + hd) : -INFINITY;
-                            lv[j] = __ldcg(sp + kHeads * D + kHeads + hd);
-                            ov[j] = __ldcg(reinterpret_cast<const float4*>(sp + hd * D + d4));
-                        }
-                        float nm = m;
-#pragma unroll
-                        for (int j = 0; j < kMergeGroup; ++j) nm = fmaxf(nm, mv[j]);
-                        if (nm == -INFINITY) continue;   // nothing but parts without rows so far
-                        const float c = m == -INFINITY ? 0.f : dm::fast_exp2(m - nm);
-                        l *= c; acc.x *= c; acc.y *= c; acc.z *= c; acc.w *= c;
-                        m = nm;
-#pragma unroll
-                        for (int j = 0; j < kMergeGroup; ++j) {
-                            if (mv[j] == -INFINITY) continue;
-                            const float w = dm::fast_exp2(mv[j] - m);
-                            l = fmaf(w, lv[j], l);
-                            acc.x = fmaf(w, ov[j].x, acc.x); acc.y = fmaf(w, ov[j].y, acc.y);
-                            acc.z = fmaf(w, ov[j].z, acc.z); acc.w = fmaf(w, ov[j].w, acc.w);
-                        }
-                    }
-                    store_out4(out + (hq0 + hd) * D + d4, acc, l);
-                }
-            }
-        }
-        left -= take;
-        if (left == 0) break;
+        joiner.join(me, p, nt, take, nh, D, out + hq0 * D, block_sum, block_ml);
+        me.left -= take;
+        if (me.left == 0) break;
         next_unit(line, p, nt);
         __syncthreads();   // the ring, sh_m and sh_l are written again
     }
-    zero_empty();
-    if (csize > 1 && !__all_sync(kFull, got)) {
-        // Gave up on a hand-over: the block's shared memory stays until the cluster's other blocks have left (each of their waits ends, and a
-        // thread that has left is not waited for) and what they handed over has landed.
-        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-        for (unsigned back = 1; back <= 2 && back <= turn; ++back) umma::mbar_wait<true>(smem_u32(&sh_bar[(turn - back) & 1]), (turn - back) >> 1 & 1);
-    }
+    zero_empty(pages, line, Hq, G, kHeads, D, out);
+    joiner.leave(me);
 }
 
 template <int D, bool kWhole, bool kPair>
@@ -537,23 +336,8 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
         ready[dev & 63] = own_error(cudaFuncSetAttribute(paged_decode_mma<D, kWhole, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmemBytes));
     });
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
-    const int64_t units = (int64_t)line.entries * line.per_entry;
-    int blocks = sms * Shape<D>::kBlocksPerSm;
-    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
-    // Up to 64 units: clusters of four, as many as find room at once (7/8 of the block slots: 64 of 4 x 74), and of those a multiple of the units
-    // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.0
-    // and 17, of 32 K 31.0 and 38.0, of 128 K 98 and 102; 4 units of 128 K with seven query heads 55 and 74; 16 units of 32 K 53 and 58.  Clusters
-    // of eight: 1 K rows 7.8 and 9.8 (of four), but 8 K 15.7 and 13.2, because the next launch's clusters find room only when this one is gone.
-    // From 17 units on each block stands for itself where the units are short: 32 units of 3 K rows 18.3 (clusters 21), of 25 K 81 and 81.
-    // More units: single blocks (128 units of 150 rows 12.8, in clusters of two 17.1; of 12 K rows 138 and 135; 512 of 1.5 K 73.5 and 76.2).
-    const int c = units <= 64 ? 4 : 1;
-    unsigned short_below = 0;
-    line.parties = blocks;
-    if (c > 1) {
-        line.parties = blocks * 7 / 8 / c;
-        if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
-        short_below = units <= 16 ? 0 : (unsigned)units * 512;
-    }
+    const Division part = divide(line, sms, [](int, int) { return Shape<D>::kBlocksPerSm; }, D);
+    const int c = part.cluster;
     const float scale = (a.scale == 0.f ? 1.f / sqrtf((float)a.d) : a.scale) * 1.4426950408889634f;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(line.parties * c);
@@ -567,7 +351,7 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return own_error(cudaLaunchKernelEx(&cfg, paged_decode_mma<D, kWhole, kPair>, pages_of<const bf16>(a.cache), (const bf16*)a.q, a.Hq, a.Hkv, line, short_below,
+    return own_error(cudaLaunchKernelEx(&cfg, paged_decode_mma<D, kWhole, kPair>, pages_of<const bf16>(a.cache), (const bf16*)a.q, a.Hq, a.Hkv, line, part.short_below,
                                         scale, (bf16*)a.out, (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status));
 }
 
@@ -580,11 +364,32 @@ cudaError_t start(const PagedDecodeArgs& a, const Line& line, int dev, int sms, 
 
 }  // namespace
 
+Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d) {
+    const int64_t units = (int64_t)line.entries * line.per_entry;
+    // Up to 64 units: clusters of four, as many as find room at once (7/8 of the block slots: 64 of 4 x 74), and of those a multiple of the units
+    // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.0
+    // and 17, of 32 K 31.0 and 38.0, of 128 K 98 and 102; 4 units of 128 K with seven query heads 55 and 74; 16 units of 32 K 53 and 58.  Clusters
+    // of eight: 1 K rows 7.8 and 9.8 (of four), but 8 K 15.7 and 13.2, because the next launch's clusters find room only when this one is gone.
+    // From 17 units on each block stands for itself where the units are short: 32 units of 3 K rows 18.3 (clusters 21), of 25 K 81 and 81.
+    // More units: single blocks (128 units of 150 rows 12.8, in clusters of two 17.1; of 12 K rows 138 and 135; 512 of 1.5 K 73.5 and 76.2).
+    const int c = units <= 64 ? kCluster : 1;
+    int blocks = sms * blocks_of(c, d);
+    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    unsigned short_below = 0;
+    line.parties = blocks;
+    if (c > 1) {
+        line.parties = blocks * 7 / 8 / c;
+        if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
+        short_below = units <= 16 ? 0 : (unsigned)units * 512;
+    }
+    return {c, short_below};
+}
+
 }  // namespace pg
 
 bool paged_decode_mma_supported(const PagedDecodeArgs& a) { return a.dt == SC_BF16 && (a.d == 64 || a.d == 128 || a.d == 256); }
 
-size_t paged_decode_mma_ws_bytes() { return pg::kTicketBytes + sizeof(float) * 2 * pg::kMaxBlocks * pg::Shape<256>::kPartStride; }
+size_t paged_decode_ws_bytes() { return pg::kTicketBytes + sizeof(float) * 2 * pg::kMaxBlocks * pg::part_floats(pg::kMaxD); }
 
 cudaError_t launch_paged_decode_mma(const PagedDecodeArgs& a, cudaStream_t st) {
     int dev = 0, sms = 148;

@@ -1,262 +1,321 @@
-// sc_paged_decode_attn for any type and head size (d a multiple of 8 up to 256): one pass over the rows on CUDA cores.
+// sc_paged_decode_attn for any type and head size (d a multiple of 8 up to 256): the scores and the weighted sum on CUDA cores, in fp32.
 //
-// One block takes a stretch of the launch's line of tiles (paged.cuh), for up to four query heads of a KV head at a time.  Its warps
-// take 32-row tiles of a segment in turn: a lane finds the page of one row; eight lanes per row form the scores, one
-// lane per row takes part in the online softmax in fp32, and for the weighted sum a lane owns four columns of every row.
+// The frame is the tensor-core kernel's (paged_attn.cuh): a party takes a stretch of the line of 16-row tiles, a warp's tiles come through a ring
+// of cp.async stages.  A row's 16-byte chunks lie XOR-swizzled in a place of a multiple of 128 bytes.  Scores: a lane has one of the 16
+// rows and every other chunk of it (the queries are read by broadcast), so one exchange between lanes finishes a score.  Weighted sum: a lane has
+// a chunk of columns (or two) and every row, or every R-th where a row has few chunks.  Bounded by its loads: a tile's two products take
+// 650 instructions of a warp for 16 KB (float32, d = 128, four queries).
 // Serves SC_F32 and head sizes that the tensor-core kernel does not take, and cross-checks it.
-#include "paged.cuh"
+#include <mutex>
+
+#include "paged_attn.cuh"
 
 namespace sc {
 namespace pg {
 
 namespace {
 
-constexpr int kTile = 32;
-constexpr int kHeads = 4;       // query heads per block
-constexpr int kMaxD = 256;
-constexpr int kWarps = 4;
-constexpr int kPartiesPerSm = 3;
-constexpr int kMaxParties = 160 * kPartiesPerSm;
-constexpr int kLeast = 4;       // tiles a stretch has at least: one per warp
+constexpr float kMaxSlack = 8.f;          // log2 units a score may exceed the running maximum before it is raised
 
-static_assert(kMaxParties * 4 <= (int)kTicketBytes, "a counter per party");
-
-// NC: the most 32-column pieces a row has (4 or 8).
-template <typename T, int NC>
-__global__ void __launch_bounds__(kWarps * 32)
-paged_decode_generic(const Pages<T> pages, const T* __restrict__ q, int Hq, int Hkv, int d, const Line line, float scale_log2, T* __restrict__ out,
-                     int32_t* __restrict__ tickets, float* __restrict__ part, int32_t* status) {
-    constexpr int kPer = NC / 4;
-    __shared__ __align__(16) float sq[kHeads][kMaxD];
-    __shared__ __align__(16) float4 sp[kWarps][kTile];              // scores, then weights, of a tile: [row][head]
-    __shared__ __align__(16) float so[kWarps][kHeads][kMaxD];       // the warps' sums
-    __shared__ float sm[kWarps][kHeads], sl[kWarps][kHeads];
-    __shared__ int sh_last;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, sub = lane & 7, rsub = lane >> 3;
-    in_stream_order();
-    const int G = Hq / Hkv, groups = (G + kHeads - 1) / kHeads, ps = pages.page_size;
-    const auto head_of = [&](int entry, int unit, int& b, int& h, int& g0) {
-        b = entry / pages.table_heads;
-        h = pages.table_heads > 1 ? entry - b * pages.table_heads : unit / groups;
-        g0 = unit % groups * kHeads;
-    };
-    // heads without rows
-    for (int e = blockIdx.x; e < line.entries; e += gridDim.x) {
-        if (line.len(e) > 0) continue;
-        for (int i = threadIdx.x; i < line.per_entry * kHeads * d; i += kWarps * 32) {
-            int b, h, g0;
-            const int unit = i / (kHeads * d), g = i / d % kHeads;
-            head_of(e, unit, b, h, g0);
-            if (g0 + g < G) Elem<T>::store(out + ((int64_t)b * Hq + h * G + g0 + g) * d + i % d, 0.f);
-        }
-    }
-    const unsigned total = total_of(line, lane), stretch = max((total + line.parties - 1) / line.parties, (unsigned)kLeast), from = min((uint64_t)blockIdx.x * stretch, (uint64_t)total);
-    if (from >= total) return;
-    unsigned left = min(stretch, total - from);
-    for (Place p = place_of(line, from, lane);;) {
-        const int len = line.len(p.entry), nt = line.tiles(p.entry);
-        const int take = (int)min((unsigned)(nt - p.tile), left), t_end = p.tile + take;
-        int b, h, g0;
-        head_of(p.entry, p.unit, b, h, g0);
-        const int nh = min(kHeads, G - g0), hq0 = b * Hq + h * G + g0;
-        const int32_t* table = pages.table_of(p.entry);
-        const int hp = pages.page_heads > 1 ? h : 0;
-        const T* kh = pages.k + hp * pages.head_stride;
-        const T* vh = pages.v + hp * pages.head_stride;
-        for (int i = threadIdx.x; i < kHeads * kMaxD; i += kWarps * 32) {
-            const int g = i / kMaxD, c = i % kMaxD;
-            sq[g][c] = g < nh && c < d ? Elem<T>::load(q + (int64_t)(hq0 + g) * d + c) * scale_log2 : 0.f;
-        }
-        __syncthreads();
-        float m[kHeads], l[kHeads], acc[kHeads][kPer][4];
+__device__ __forceinline__ void unpack(const uint4& w, float (&x)[8]) {
+    const uint32_t a[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int g = 0; g < kHeads; ++g) {
-            m[g] = -INFINITY; l[g] = 0.f;   // l: this lane's rows only
-#pragma unroll
-            for (int u = 0; u < kPer; ++u) acc[g][u][0] = acc[g][u][1] = acc[g][u][2] = acc[g][u][3] = 0.f;
-        }
-        for (int t = p.tile + w; t < t_end; t += kWarps) {
-            const int row = t * kTile + lane;
-            int64_t at = -1;   // where this lane's row lies
-            float lc = 0.f;    // ln s, in base-2 units
-            if (row < len) {
-                const int slot = row / ps, id = table[slot];
-                if (pages.names_page(id)) {
-                    at = id * pages.page_stride + (int64_t)(row - slot * ps) * pages.row_stride;
-                    if (pages.count != nullptr) lc = log2f((float)max(pages.count[((int64_t)id * pages.page_heads + hp) * ps + (row - slot * ps)], 1));
-                } else {
-                    set_status(status, SC_ERR_INVALID_ARG);
-                }
-            }
-            const unsigned rows_ok = __ballot_sync(kFull, at >= 0);
-#pragma unroll (16 / NC)
-            for (int it = 0; it < 8; ++it) {   // four rows at a time
-                const int r = it * 4 + rsub;
-                const int64_t ra = __shfl_sync(kFull, at, r);
-                float4 kv[NC];
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int col = (c * 8 + sub) * 4;
-                    kv[c] = ra >= 0 && col < d ? load4(kh + ra + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-                float s[kHeads];
-#pragma unroll
-                for (int g = 0; g < kHeads; ++g) {
-                    s[g] = 0.f;
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        const float4 qv = *reinterpret_cast<const float4*>(&sq[g][(c * 8 + sub) * 4]);
-                        s[g] = fmaf(qv.x, kv[c].x, fmaf(qv.y, kv[c].y, fmaf(qv.z, kv[c].z, fmaf(qv.w, kv[c].w, s[g]))));
-                    }
-                }
-#pragma unroll
-                for (int o = 1; o < 8; o <<= 1)
-#pragma unroll
-                    for (int g = 0; g < kHeads; ++g) s[g] += __shfl_xor_sync(kFull, s[g], o);
-                if (sub == 0) sp[w][r] = make_float4(s[0], s[1], s[2], s[3]);
-            }
-            __syncwarp();
-            {
-                const float4 xs = sp[w][lane];
-                const float x[kHeads] = {xs.x, xs.y, xs.z, xs.w};
-                float pw[kHeads];
-#pragma unroll
-                for (int g = 0; g < kHeads; ++g) {
-                    const float xg = rows_ok >> lane & 1 ? x[g] + lc : -INFINITY;
-                    const float mn = fmaxf(m[g], warp_max(xg)), ref = mn == -INFINITY ? 0.f : mn;   // (no row so far)
-                    const float corr = exp2f(m[g] - ref);
-                    pw[g] = exp2f(xg - ref);
-                    l[g] = l[g] * corr + pw[g];
-#pragma unroll
-                    for (int u = 0; u < kPer; ++u) { acc[g][u][0] *= corr; acc[g][u][1] *= corr; acc[g][u][2] *= corr; acc[g][u][3] *= corr; }
-                    m[g] = mn;
-                }
-                __syncwarp();
-                sp[w][lane] = make_float4(pw[0], pw[1], pw[2], pw[3]);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int r0 = 0; r0 < kTile; r0 += 16) {   // sixteen rows requested together
-                if ((rows_ok >> r0 & 0xffff) == 0) continue;
-#pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int col = (u * 32 + lane) * 4;
-                    float4 vv[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int64_t ra = __shfl_sync(kFull, at, r0 + j);
-                        vv[j] = ra >= 0 && col < d ? load4(vh + ra + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float4 pv = sp[w][r0 + j];
-                        const float pgv[kHeads] = {pv.x, pv.y, pv.z, pv.w};
-#pragma unroll
-                        for (int g = 0; g < kHeads; ++g) {
-                            acc[g][u][0] = fmaf(pgv[g], vv[j].x, acc[g][u][0]); acc[g][u][1] = fmaf(pgv[g], vv[j].y, acc[g][u][1]);
-                            acc[g][u][2] = fmaf(pgv[g], vv[j].z, acc[g][u][2]); acc[g][u][3] = fmaf(pgv[g], vv[j].w, acc[g][u][3]);
-                        }
-                    }
-                }
-            }
-            __syncwarp();   // the next tile's scores overwrite the weights
-        }
-        // the warps' (m, l, O), in order
-#pragma unroll
-        for (int g = 0; g < kHeads; ++g) {
-            const float lw = warp_sum(l[g]);
-            if (lane == 0) { sm[w][g] = m[g]; sl[w][g] = lw; }
-#pragma unroll
-            for (int u = 0; u < kPer; ++u) {
-                const int col = (u * 32 + lane) * 4;
-                *reinterpret_cast<float4*>(&so[w][g][col]) = make_float4(acc[g][u][0], acc[g][u][1], acc[g][u][2], acc[g][u][3]);
-            }
-        }
-        __syncthreads();
-        const bool whole = take == nt;
-        const int part_stride = kHeads * (d + 2);
-        float* mine = part + (size_t)(2 * blockIdx.x + (p.at > from)) * part_stride;   // [head][d columns, m, l]
-        for (int i = threadIdx.x; i < nh * d; i += kWarps * 32) {
-            const int g = i / d, c = i - g * d;
-            float mm = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < kWarps; ++j) mm = fmaxf(mm, sm[j][g]);
-            float ls = 0.f, o = 0.f;
-#pragma unroll
-            for (int j = 0; j < kWarps; ++j) {
-                const float f = sm[j][g] == -INFINITY ? 0.f : exp2f(sm[j][g] - mm);   // 0: a warp without rows
-                ls += f * sl[j][g];
-                o = fmaf(f, so[j][g][c], o);
-            }
-            if (whole) {
-                Elem<T>::store(out + (int64_t)(hq0 + g) * d + c, ls != 0.f ? o / ls : 0.f);
-            } else {
-                mine[g * (d + 2) + c] = o;
-                if (c == 0) { mine[g * (d + 2) + d] = mm; mine[g * (d + 2) + d + 1] = ls; }
-            }
-        }
-        if (!whole) {
-            const unsigned first = p.at / stretch, last = (p.at + nt - 1) / stretch;
-            int32_t* ticket = tickets + first;   // (a party begins one shared unit at most)
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int t;
-                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(t) : "l"(ticket) : "memory");
-                sh_last = t == (int)(last - first);
-                if (sh_last) *ticket = 0;   // ready for the next call
-            }
-            __syncthreads();
-            if (sh_last) {
-                for (int i = threadIdx.x; i < nh * d; i += kWarps * 32) {
-                    const int g = i / d, c = i - g * d;
-                    float mm = -INFINITY, ls = 0.f, o = 0.f;
-                    for (unsigned j = first; j <= last; ++j) {
-                        const float* from_j = part + (size_t)(2 * j + (p.at > j * stretch)) * part_stride + g * (d + 2);
-                        const float mj = __ldcg(from_j + d), lj = __ldcg(from_j + d + 1), oj = __ldcg(from_j + c);
-                        const float mn = fmaxf(mm, mj), ref = mn == -INFINITY ? 0.f : mn;
-                        const float c0 = exp2f(mm - ref), c1 = exp2f(mj - ref);
-                        ls = ls * c0 + lj * c1;
-                        o = o * c0 + oj * c1;
-                        mm = mn;
-                    }
-                    Elem<T>::store(out + (int64_t)(hq0 + g) * d + c, ls != 0.f ? o / ls : 0.f);
-                }
-            }
-        }
-        left -= take;
-        if (left == 0) return;
-        next_unit(line, p, nt);
-        __syncthreads();   // sq, so, sm, sl are written again
-    }
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void unpack(const uint4& w, float (&x)[4]) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
 }
 
-template <typename T>
-cudaError_t run(const PagedDecodeArgs& a, cudaStream_t st) {
+__host__ __device__ inline int pitch_of(int d, int esize) { return (d * esize + 127) / 128 * 128; }
+__host__ __device__ inline int stage_bytes(int pitch) { return 2 * kTile * pitch + 80; }   // K, V, 16 counts, which rows count
+
+// What an SM holds at once hides the latency of the steps of one warp: three blocks, two with eight query heads, and a ring that leaves room for
+// them (rows of 512 bytes: one stage, 16 sequences x 8 heads x 4 K rows of float32 108 us, with three stages and one block per SM 186).
+__host__ __device__ constexpr int blocks_by_registers(int heads) { return heads <= 4 ? 3 : 2; }
+__host__ __device__ constexpr int stages_of(int pitch) { return pitch <= 128 ? 3 : pitch <= 256 ? 2 : 1; }
+
+// kH: query heads of a unit.  kStages: of a warp's ring.  kChunks: a lane's chunks of columns.
+template <typename T, int kH, int kStages, int kChunks>
+__global__ void __launch_bounds__(kThreads, blocks_by_registers(kH))
+paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq, int Hkv, int d, Line line, unsigned short_below, float scale_log2,
+                     T* __restrict__ out, int32_t* __restrict__ tickets, float* __restrict__ part, int32_t* status) {
+    constexpr int E = 16 / sizeof(T);
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int pitch = pitch_of(d, sizeof(T)), stage_size = stage_bytes(pitch), ring_size = kWarps * kStages * stage_size;
+    float* sq = reinterpret_cast<float*>(smem + ring_size);                             // queries [kH][d]
+    __shared__ __align__(16) float sp[kWarps][kTile][kH];                              // weights of a tile
+    __shared__ float sh_m[kWarps][kHeads], sh_l[kWarps][kHeads];
+    __shared__ int sh_last;
+    __shared__ __align__(8) unsigned long long sh_bar[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Party me;
+    me.set_up(sh_bar);
+    in_stream_order();
+    const int G = Hq / Hkv;
+    if (!me.plan(line, short_below, lane)) {
+        zero_empty(pages, line, Hq, G, kH, d, out);
+        me.step();
+        return;
+    }
+    Joiner joiner = {sh_bar, smem + ring_size + kH * d * 4, &sh_last, tickets, part, status, kH, 0u, true};
+    const int chunks = d / E;                            // of a row
+    int width = 2;                                       // lanes that a row's chunks are spread over (a tile has 16 rows)
+    while (width < chunks && width < 32) width *= 2;
+    const int c0 = lane % width, v0 = lane / width, step = 32 / width;
+    const uint32_t ring = smem_u32(smem) + warp * (kStages * stage_size);
+    const unsigned char* ring_p = smem + warp * (kStages * stage_size);
+
+    for (Place p = me.begin(line, lane);;) {
+        const int len = line.len(p.entry), nt = line.tiles(p.entry);
+        const int take = (int)min((unsigned)(nt - p.tile), me.left);
+        const Unit unit(pages, p.entry, p.unit, G, kH);
+        const int64_t hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
+        const int each = (take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, take), t1 = p.tile + min((me.crank + 1) * each, take);
+        const int my_tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
+        const int hp = pages.page_heads > 1 ? unit.h : 0;
+        const T* kh = pages.k + hp * pages.head_stride;
+        const T* vh = pages.v + hp * pages.head_stride;
+        const int32_t* count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
+        Finder<false> finder = {pages.table_of(p.entry), pages.page_size, len, t0 + warp, my_tiles, {}, {}};
+        finder.start(lane);
+        const auto copy = [&](int stage_no, int j) {
+            const uint32_t stage = ring + stage_no * stage_size;
+            const int2 at = finder.get(j, lane);
+            const bool page = pages.names_page(at.x);
+            const int64_t mine = page ? at.x * pages.page_stride + (int64_t)at.y * pages.row_stride : -1;
+            const unsigned rows_ok = __ballot_sync(kFull, page) & 0xffff;
+            for (int r0 = 0; r0 < kTile; r0 += step) {
+                const int r = r0 + v0;
+                const int64_t o = __shfl_sync(kFull, mine, r);
+                const uint32_t row = stage + r * pitch;
+#pragma unroll
+                for (int n = 0; n < kChunks; ++n) {
+                    const int c = c0 + n * 32;
+                    if (c >= chunks) continue;
+                    const uint32_t to = row + ((c ^ (r & 7)) << 4);
+                    cp_async16(to, o >= 0 ? (const void*)(kh + o + c * E) : q, o >= 0 ? 16 : 0);
+                    cp_async16(to + kTile * pitch, o >= 0 ? (const void*)(vh + o + c * E) : q, o >= 0 ? 16 : 0);
+                }
+            }
+            if (count != nullptr && lane < kTile) {
+                const int64_t o = (int64_t)at.x * pages.page_heads * pages.page_size + at.y;
+                cp_async4(stage + 2 * kTile * pitch + lane * 4, page ? (const void*)(count + o) : q, page ? 4 : 0);
+            }
+            if (lane == 0) asm volatile("st.shared.u32 [%0], %1;\n" ::"r"(stage + 2 * kTile * pitch + 64), "r"(rows_ok) : "memory");
+            if (!page && (t0 + warp + j * kWarps) * kTile + (lane & 15) < len) set_status(status, SC_ERR_INVALID_ARG);
+        };
+#pragma unroll
+        for (int s = 0; s < kStages; ++s) {
+            if (s < my_tiles) copy(s, s);
+            cp_async_commit();
+        }
+        for (int i = threadIdx.x; i < kH * d; i += kThreads) {
+            const int g = i / d;
+            sq[i] = g < unit.nh ? Elem<T>::load(q + hq0 * d + i) : 0.f;
+        }
+        __syncthreads();
+        float m[kH], l[kH], acc[kH][kChunks][E];
+#pragma unroll
+        for (int g = 0; g < kH; ++g) {
+            m[g] = -INFINITY; l[g] = 0.f;   // l: this lane's rows only
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[g][n][e] = 0.f;
+        }
+        int at_stage = 0;
+        for (int i = 0; i < my_tiles; ++i) {
+            cp_async_wait<kStages - 1>();
+            __syncwarp();
+            const unsigned char* st = ring_p + at_stage * stage_size;
+            const int r = lane & 15;
+            const bool ok = *reinterpret_cast<const unsigned*>(st + 2 * kTile * pitch + 64) >> r & 1;
+            float4 s[kH];   // four sums a score: short chains of roundings
+#pragma unroll
+            for (int g = 0; g < kH; ++g) s[g] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int c = lane >> 4; c < chunks; c += 2) {
+                float kv[E];
+                unpack(*reinterpret_cast<const uint4*>(st + r * pitch + ((c ^ (r & 7)) << 4)), kv);
+#pragma unroll
+                for (int g = 0; g < kH; ++g)
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) {
+                        const float4 qv = *reinterpret_cast<const float4*>(sq + g * d + c * E + e);
+                        const float2 a = umma::fma2(make_float2(qv.x, qv.y), make_float2(kv[e], kv[e + 1]), make_float2(s[g].x, s[g].y));
+                        const float2 b = umma::fma2(make_float2(qv.z, qv.w), make_float2(kv[e + 2], kv[e + 3]), make_float2(s[g].z, s[g].w));
+                        s[g] = make_float4(a.x, a.y, b.x, b.y);
+                    }
+            }
+            float x[kH];
+            // ln s, in base-2 units (a valid row has count >= 1)
+            const float lc = count != nullptr ? log2f((float)max(reinterpret_cast<const int*>(st + 2 * kTile * pitch)[r], 1)) : 0.f;
+            bool higher = false;
+#pragma unroll
+            for (int g = 0; g < kH; ++g) {
+                x[g] = (s[g].x + s[g].y) + (s[g].z + s[g].w);
+                x[g] += __shfl_xor_sync(kFull, x[g], 16);
+                x[g] = ok ? fmaf(x[g], scale_log2, lc) : -INFINITY;
+                higher |= x[g] > m[g] + kMaxSlack;
+            }
+            if (__any_sync(kFull, higher)) {
+#pragma unroll
+                for (int g = 0; g < kH; ++g) {
+                    float mx = x[g];
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
+                    const float mn = fmaxf(m[g], mx), f = mn == -INFINITY ? 1.f : exp2f(m[g] - mn);
+                    l[g] *= f;
+#pragma unroll
+                    for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) acc[g][n][e] *= f;
+                    m[g] = mn;
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < kH; ++g) {
+                const float w = exp2f(x[g] - (m[g] == -INFINITY ? 0.f : m[g]));
+                if (lane < 16) { l[g] += w; sp[warp][r][g] = w; }
+            }
+            __syncwarp();
+#pragma unroll 4
+            for (int r0 = 0; r0 < kTile; r0 += step) {
+                const int vr = r0 + v0;
+                float w[kH];
+#pragma unroll
+                for (int g = 0; g < kH; g += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(&sp[warp][vr][g]);
+                    w[g] = t.x; w[g + 1] = t.y; w[g + 2] = t.z; w[g + 3] = t.w;
+                }
+#pragma unroll
+                for (int n = 0; n < kChunks; ++n) {
+                    const int c = c0 + n * 32;
+                    if (c >= chunks) continue;
+                    float vv[E];
+                    unpack(*reinterpret_cast<const uint4*>(st + (kTile + vr) * pitch + ((c ^ (vr & 7)) << 4)), vv);
+#pragma unroll
+                    for (int g = 0; g < kH; ++g)
+#pragma unroll
+                        for (int e = 0; e < E; e += 2) {
+                            const float2 a = umma::fma2(make_float2(w[g], w[g]), make_float2(vv[e], vv[e + 1]), make_float2(acc[g][n][e], acc[g][n][e + 1]));
+                            acc[g][n][e] = a.x; acc[g][n][e + 1] = a.y;
+                        }
+                }
+            }
+            __syncwarp();
+            if (i + kStages < my_tiles) copy(at_stage, i + kStages);   // the stage just consumed takes the next tile
+            cp_async_commit();
+            at_stage = at_stage + 1 == kStages ? 0 : at_stage + 1;
+        }
+        cp_async_wait<0>();
+
+        // ---- the warps of this block meet (fixed order) ----
+#pragma unroll
+        for (int g = 0; g < kH; ++g) {
+            const float lw = warp_sum(l[g]);
+            if (lane == 0) { sh_m[warp][g] = m[g]; sh_l[warp][g] = lw; }
+        }
+        if (kH < kHeads && lane < kHeads - kH) { sh_m[warp][kH + lane] = -INFINITY; sh_l[warp][kH + lane] = 0.f; }
+        __syncthreads();   // every warp is done with its ring; reuse it as [warp][kH][d] fp32
+        float* slabs = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int g = 0; g < kH; ++g) {
+            float bm = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) bm = fmaxf(bm, sh_m[w][g]);
+            const float f = m[g] == -INFINITY ? 0.f : exp2f(m[g] - bm);
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float a = acc[g][n][e];
+                    for (int o = width; o < 32; o <<= 1) a += __shfl_xor_sync(kFull, a, o);   // the lanes that share a chunk
+                    const int c = c0 + n * 32;
+                    if (v0 == 0 && c < chunks) slabs[(warp * kH + g) * d + c * E + e] = a * f;
+                }
+        }
+        __syncthreads();
+        const auto block_sum = [&](int e4) {   // four columns of a head
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float4 v = *reinterpret_cast<const float4*>(slabs + w * kH * d + e4 * 4);
+                a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+            }
+            return a;
+        };
+        const auto block_ml = [&](int g) {
+            float bm = -INFINITY, bl = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) bm = fmaxf(bm, sh_m[w][g]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) bl += sh_m[w][g] == -INFINITY ? 0.f : sh_l[w][g] * exp2f(sh_m[w][g] - bm);
+            return make_float2(bm, bl);
+        };
+        joiner.join(me, p, nt, take, unit.nh, d, out + hq0 * d, block_sum, block_ml);
+        me.left -= take;
+        if (me.left == 0) break;
+        next_unit(line, p, nt);
+        __syncthreads();   // the ring, sq, sh_m and sh_l are written again
+    }
+    zero_empty(pages, line, Hq, G, kH, d, out);
+    joiner.leave(me);
+}
+
+template <typename T, int kH, int kStages>
+int bytes_of(int cluster, int d) { return kWarps * kStages * stage_bytes(pitch_of(d, sizeof(T))) + kH * d * 4 + (cluster > 1 ? 2 * recv_bytes(d, kH) : 0); }
+
+template <typename T, int kH, int kStages, int kChunks>
+cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
     int dev = 0, sms = 148;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    const Pages<T> pages = pages_of<T>(a.cache);
-    const int groups = div_up(a.Hq / a.Hkv, kHeads);
+    static std::once_flag once[64];   // per device
+    static cudaError_t ready[64];
+    const auto kernel = paged_decode_generic<T, kH, kStages, kChunks>;
+    constexpr int kMost = kChunks * 32 * 16 / (int)sizeof(T) < kMaxD ? kChunks * 32 * 16 / (int)sizeof(T) : kMaxD;   // d
+    std::call_once(once[dev & 63], [&] { ready[dev & 63] = own_error(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_of<T, kH, kStages>(4, kMost))); });
+    if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
     Line line;
-    line.lens = a.lens; line.entries = a.B * a.cache.table_heads; line.per_entry = a.Hkv / a.cache.table_heads * groups;
-    line.cap = pages.cap(); line.tile = kTile;
-    line.parties = sms * kPartiesPerSm < kMaxParties ? sms * kPartiesPerSm : kMaxParties;
+    line.lens = a.lens; line.entries = a.B * a.cache.table_heads; line.per_entry = a.Hkv / a.cache.table_heads * div_up(a.Hq / a.Hkv, kH);
+    line.cap = a.cache.max_pages * a.cache.page_size; line.tile = kTile;
+    const Division part = divide(line, sms, [](int cluster, int d) {
+        const int room = 228 * 1024 / (bytes_of<T, kH, kStages>(cluster, d) + 2560 + (kH > 4 ? 1024 : 0));
+        return room < 1 ? 1 : room < blocks_by_registers(kH) ? room : blocks_by_registers(kH);
+    }, a.d);
     const float scale = (a.scale == 0.f ? 1.f / sqrtf((float)a.d) : a.scale) * 1.4426950408889634f;
-    return launch_in_order(a.d <= 128 ? paged_decode_generic<T, 4> : paged_decode_generic<T, 8>, dim3(line.parties), kWarps * 32, 0, st, pages,
-                           (const T*)a.q, a.Hq, a.Hkv, a.d, line, scale, (T*)a.out, (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(line.parties * part.cluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes_of<T, kH, kStages>(part.cluster, a.d);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = part.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return own_error(cudaLaunchKernelEx(&cfg, kernel, pages_of<const T>(a.cache), (const T*)a.q, a.Hq, a.Hkv, a.d, line, part.short_below, scale, (T*)a.out,
+                                        (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status));
+}
+
+template <int kH>
+cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
+    typedef __nv_bfloat16 bf16;
+    const int stages = stages_of(pitch_of(a.d, a.dt == SC_BF16 ? 2 : 4));
+    if (a.dt == SC_BF16) return stages == 3 ? start<bf16, kH, 3, 1>(a, st) : stages == 2 ? start<bf16, kH, 2, 1>(a, st) : start<bf16, kH, 1, 1>(a, st);
+    if (a.d > 128) return start<float, kH, 1, 2>(a, st);
+    return stages == 3 ? start<float, kH, 3, 1>(a, st) : stages == 2 ? start<float, kH, 2, 1>(a, st) : start<float, kH, 1, 1>(a, st);
 }
 
 }  // namespace
 
 }  // namespace pg
 
-size_t paged_decode_generic_ws_bytes(int32_t d) {
-    return pg::kTicketBytes + sizeof(float) * 2 * pg::kMaxParties * pg::kHeads * ((size_t)d + 2);
-}
-
 cudaError_t launch_paged_decode_generic(const PagedDecodeArgs& a, cudaStream_t st) {
-    const cudaError_t e = a.dt == SC_BF16 ? pg::run<__nv_bfloat16>(a, st) : pg::run<float>(a, st);
+    const cudaError_t e = a.Hq / a.Hkv <= 4 ? pg::start<4>(a, st) : pg::start<8>(a, st);
     if (e == cudaSuccess) note_launches(1);
     return e;
 }

@@ -46,9 +46,15 @@ def rows_of(t, table, n, h, ps):
     return t[ids, h].reshape(-1, *t.shape[3:])[:n].double()
 
 
-def attention(q, k, v, table, lens, scale=0.0, count=None):
-    """q [B, Hq, d]; k, v [P, heads, ps, d]; table [B, th, W]; lens [B, th].  Eq. 4 row by row of the batch, in 64 bits."""
+def attention(q, k, v, table, lens, scale=0.0, count=None, rounding=False):
+    """q [B, Hq, d]; k, v [P, heads, ps, d]; table [B, th, W]; lens [B, th].  Eq. 4 row by row of the batch, in 64 bits.
+
+    ``rounding``: also what scores in fp32 can be off by, as a bound on each output's error.  A sum of d products in any order, each of them
+    in at most d roundings, is off by at most d 2^-24 sum |q_c k_tc|; the score made of it is rounded twice more: delta_t.  Weights
+    w_t exp(e_t) with |e_t| <= delta_t move sum w v / sum w by sum p_t |e_t| |v_t - out| to first order (p = w / sum w); doubled for what
+    is left of the series (delta < 1/2 here)."""
     B, Hq, d = q.shape
+    bound = torch.zeros((B, Hq, d), dtype=torch.float64)
     heads, ps, th = k.shape[1], k.shape[2], table.shape[1]
     Hkv = max(heads, th)
     G = Hq // Hkv
@@ -65,8 +71,15 @@ def attention(q, k, v, table, lens, scale=0.0, count=None):
             if count is not None:
                 x = x + rows_of(count, table[b, t], n, hp, ps).log()
             w = torch.exp(x - x.amax(1, keepdim=True))
-            out[b, h * G:(h + 1) * G] = w @ vv / w.sum(1, keepdim=True)
-    return out
+            o = w @ vv / w.sum(1, keepdim=True)
+            out[b, h * G:(h + 1) * G] = o
+            if rounding:
+                qq, sc = q[b, h * G:(h + 1) * G].double(), scale if scale else 1.0 / math.sqrt(d)
+                delta = d * 2.0 ** -24 * sc * (qq.abs() @ kk.abs().T) + 2.0 ** -23 * x.abs()
+                assert float((delta * (w > 1e-12)).max()) < 0.5
+                p = w / w.sum(1, keepdim=True) * delta
+                bound[b, h * G:(h + 1) * G] = 2 * torch.einsum("gt,gtc->gc", p, (vv.unsqueeze(0) - o.unsqueeze(1)).abs())
+    return (out, bound) if rounding else out
 
 
 def select(q, k_min, k_max, table, lens, ps, keep, n_first, n_last):

@@ -48,7 +48,8 @@ def _check(dtype, B, Hkv, G, d, ps, lens, layout="hnd", own_pages=False, count=F
     gen = torch.Generator().manual_seed(seed + 1)
     q = (torch.randn((B, Hkv * G, d), generator=gen) * q_scale).to(dtype)
     ln = torch.tensor(lens, dtype=torch.int32)
-    want = pp.attention(q, k, v, table, ln, scale, cnt)
+    # large scores: what fp32 sums of that size can be off by is allowed beside the usual tolerance (see pp.attention)
+    want, bound = pp.attention(q, k, v, table, ln, scale, cnt, rounding=True) if q_scale != 1.0 else (pp.attention(q, k, v, table, ln, scale, cnt), 0.0)
     status = pp.status_word()
     ws = binding.paged_decode_workspace(B, Hkv * G, Hkv, d, DEV)
     cache = _device(k, v, table, cnt, layout)
@@ -56,7 +57,9 @@ def _check(dtype, B, Hkv, G, d, ps, lens, layout="hnd", own_pages=False, count=F
     pp.ok(status)
     assert pp.same_bits(*runs)                                   # a fixed order
     assert int(ws[:4096].count_nonzero()) == 0                   # its counters are left as they were
-    assert_close_vectors(runs[0].double().cpu().numpy(), want.numpy(), TOL[dtype], "attention")
+    got = runs[0].double().cpu()
+    got = want + torch.sign(got - want) * ((got - want).abs() - bound).clamp(min=0.0)
+    assert_close_vectors(got.numpy(), want.numpy(), TOL[dtype], "attention")
     empty = [(b, h) for b in range(B) for h in range(Hkv) if lens[b][h if len(lens[b]) > 1 else 0] == 0]
     for b, h in empty:
         assert int(runs[0][b, h * G:(h + 1) * G].count_nonzero()) == 0
