@@ -18,6 +18,7 @@ constexpr int kMaxBlocks = 448;           // of a launch
 constexpr int kCluster = 4;               // blocks of a party, where it is a cluster
 constexpr int kMergeGroup = 8;            // partial sums read together
 constexpr unsigned kShortStretch = 64;    // tiles per block below which stretches are cut at the units' ends
+constexpr unsigned kLongStretch = 200;    // tiles per SM from which one block on each is better than two
 constexpr int kLeast = 2;                 // tiles per warp that a stretch has at least
 constexpr int kMaxD = 256;
 __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * kHeads; }   // a partial sum: acc[8][d], m[8], l[8]
@@ -138,6 +139,13 @@ __device__ __forceinline__ void next_unit(const Line& line, Place& p, int tiles_
     do ++p.entry; while (line.tiles(p.entry) == 0);
 }
 
+// How a launch is divided: into parties of clusters of `cluster` blocks.  A line of fewer tiles than short_below: each block of a cluster stands
+// for itself.  One of long_from or more: the first long_parties only.  blocks_of(cluster): blocks that an SM holds; one_per_sm: whether long lines
+// are better off with one block on each SM.
+struct Division { int cluster; unsigned short_below, long_from; int long_parties; };
+Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d, bool one_per_sm);
+static_assert(kCluster <= dm::kMaxCluster, "");
+
 // A party as one of its blocks sees it.
 struct Party {
     int csize, crank, party;     // blocks of the party, this one's rank, the party's number
@@ -165,14 +173,15 @@ struct Party {
         if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
         in_step = true;
     }
-    // Whether the block has anything to do.  A line of fewer tiles than short_below: each block of a cluster for itself.
-    __device__ __forceinline__ bool plan(Line& line, unsigned short_below, int lane) {
+    // Whether the block has anything to do.
+    __device__ __forceinline__ bool plan(Line& line, const Division& how, int lane) {
         const unsigned total = total_of(line, lane);
-        if (total < short_below) {
+        if (total < how.short_below) {
             step();
             csize = 1; crank = 0; party = blockIdx.x;
             line.parties = gridDim.x;
         }
+        if (total >= how.long_from) line.parties = how.long_parties;
         stretch = max((total + line.parties - 1) / line.parties, (unsigned)(csize * kWarps * kLeast));
         cut = stretch < kShortStretch * csize && line.entries <= kCutEntries && line.entries * line.per_entry <= line.parties;
         from = 0;
@@ -378,12 +387,6 @@ struct Joiner {
         for (unsigned back = 1; back <= 2 && back <= turn; ++back) umma::mbar_wait<true>(smem_u32(&bar[(turn - back) & 1]), (turn - back) >> 1 & 1);
     }
 };
-
-// How a launch is divided: parties of clusters of `cluster` blocks, and the line below which each block stands for itself.  blocks_of(cluster):
-// blocks that an SM holds.
-static_assert(kCluster <= dm::kMaxCluster, "");
-struct Division { int cluster; unsigned short_below; };
-Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d);
 
 }  // namespace pg
 }  // namespace sc

@@ -30,7 +30,7 @@ struct Shape {
     static constexpr int kBlocksPerSm = D == 256 ? 1 : 2;
     static constexpr int kRowBytes = D * 2;
     static constexpr int kTileBytes = kTile * kRowBytes;             // of K or V
-    static constexpr int kStageBytes = 2 * kTileBytes + 80;          // K, V, 16 counts, which rows count
+    static constexpr int kStageBytes = 2 * kTileBytes + 64;          // K, V, 16 counts
     static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
     static constexpr int kSmemBytes = kRingBytes + 2 * recv_bytes(D, kHeads);
     static_assert(kWarps * kHeads * D * 4 <= kRingBytes, "the warps' sums lie in the ring's place");
@@ -74,66 +74,69 @@ struct Rows {
     int num_pages, len;
     int32_t* status;
 
-    __device__ __forceinline__ void copy(uint32_t stage, int tile, int2 at, int lane) const {
+    // Where a tile lies, worked out before its stage is free (the lookup and the 64-bit products take as long as a product's step).
+    struct Tile {
+        int64_t first;      // kWhole: of the lane's first chunk, in elements; else of row lane & 15, or -1
+        int64_t count;      // of the lane's count
+        unsigned rows_ok;
+    };
+    __device__ __forceinline__ Tile locate(int tile, int2 at, int lane) const {
+        constexpr int kChunks = D / 8;
+        const bool page = (unsigned)at.x < (unsigned)num_pages;
+        Tile t;
+        if (kWhole) {
+            const int rows = page ? min(kTile, len - tile * kTile) : 0;
+            t.rows_ok = (1u << rows) - 1;
+            t.first = at.x * page_stride + (int64_t)(at.y + lane / kChunks) * row_stride + lane % kChunks * 8;
+        } else {
+            t.rows_ok = __ballot_sync(kFull, page) & 0xffff;
+            t.first = page ? at.x * page_stride + (int64_t)at.y * row_stride : -1;
+        }
+        t.count = at.x * count_page + at.y + (kWhole ? lane : 0);
+        if (!page && tile * kTile + (kWhole ? 0 : lane & 15) < len) set_status(status, SC_ERR_INVALID_ARG);
+        return t;
+    }
+    __device__ __forceinline__ void copy(uint32_t stage, const Tile& t, int lane) const {
         constexpr int kChunks = D / 8, kStep = 32 / kChunks, kN = kTile / kStep;   // lanes per row, rows per round, rounds
         using S = Shape<D>;
         const int c = lane % kChunks, r0 = lane / kChunks;
-        const bool page = (unsigned)at.x < (unsigned)num_pages;
         const uint32_t dst = stage + r0 * S::kRowBytes;
-        unsigned rows_ok;
-        if (kWhole) {
-            const int rows = page ? min(kTile, len - tile * kTile) : 0;
-            rows_ok = (1u << rows) - 1;
-            const int64_t first = at.x * page_stride + (int64_t)(at.y + r0) * row_stride + c * 8;
-            if (rows == kTile) {
-                const bf16* ks = k + first;
-                const bf16* vs = v + first;
-#pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
-                    cp_async16(to, ks, 16);
-                    cp_async16(to + S::kTileBytes, vs, 16);
-                    ks += kStep * row_stride; vs += kStep * row_stride;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
-                    const bool ok = i * kStep + r0 < rows;
-                    const int64_t o = first + (int64_t)i * kStep * row_stride;
-                    cp_async16(to, ok ? (const void*)(k + o) : nowhere, ok ? 16 : 0);
-                    cp_async16(to + S::kTileBytes, ok ? (const void*)(v + o) : nowhere, ok ? 16 : 0);
-                }
-            }
-        } else {
-            const int64_t mine = page ? at.x * page_stride + (int64_t)at.y * row_stride : -1;
-            rows_ok = __ballot_sync(kFull, page) & 0xffff;
+        if (kWhole && t.rows_ok == 0xffff) {
+            const bf16* ks = k + t.first;
+            const bf16* vs = v + t.first;
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
                 const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
-                const int64_t o = __shfl_sync(kFull, mine, i * kStep + r0);
-                cp_async16(to, o >= 0 ? (const void*)(k + o + c * 8) : nowhere, o >= 0 ? 16 : 0);
-                cp_async16(to + S::kTileBytes, o >= 0 ? (const void*)(v + o + c * 8) : nowhere, o >= 0 ? 16 : 0);
+                cp_async16(to, ks, 16);
+                cp_async16(to + S::kTileBytes, vs, 16);
+                ks += kStep * row_stride; vs += kStep * row_stride;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                const uint32_t to = dst + i * kStep * S::kRowBytes + ((c ^ ((i * kStep + r0) & 7)) << 4);
+                const bool ok = t.rows_ok >> (i * kStep + r0) & 1;
+                const int64_t o = kWhole ? t.first + (int64_t)i * kStep * row_stride : __shfl_sync(kFull, t.first, i * kStep + r0) + c * 8;
+                cp_async16(to, ok ? (const void*)(k + o) : nowhere, ok ? 16 : 0);
+                cp_async16(to + S::kTileBytes, ok ? (const void*)(v + o) : nowhere, ok ? 16 : 0);
             }
         }
         if (count != nullptr && lane < kTile) {
-            const bool ok = rows_ok >> lane & 1;
-            const int64_t o = at.x * count_page + at.y + (kWhole ? lane : 0);
-            cp_async4(stage + 2 * S::kTileBytes + lane * 4, ok ? (const void*)(count + o) : nowhere, ok ? 4 : 0);
+            const bool ok = t.rows_ok >> lane & 1;
+            cp_async4(stage + 2 * S::kTileBytes + lane * 4, ok ? (const void*)(count + t.count) : nowhere, ok ? 4 : 0);
         }
-        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;\n" ::"r"(stage + 2 * S::kTileBytes + 64), "r"(rows_ok) : "memory");
-        if (!page && tile * kTile + (kWhole ? 0 : lane & 15) < len) set_status(status, SC_ERR_INVALID_ARG);
     }
 };
 
 // kPair: up to four query heads (see above).
 template <int D, bool kWhole, bool kPair>
 __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocksPerSm)
-paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int Hq, int Hkv, Line line, unsigned short_below, float scale_log2,
+paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int Hq, int Hkv, Line line, const Division how, float scale_log2,
                  bf16* __restrict__ out, int32_t* __restrict__ tickets, float* __restrict__ part, int32_t* status) {
     using S = Shape<D>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float sh_m[kWarps][kHeads], sh_l[kWarps][kHeads];
+    __shared__ unsigned sh_rows[kWarps][8];    // which rows of a warp's tiles count, by turns
     __shared__ int sh_last;
     __shared__ __align__(8) unsigned long long sh_bar[2];   // what the cluster's blocks hand this one, segments by turns
 
@@ -142,7 +145,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
     me.set_up(sh_bar);
     in_stream_order();
     const int G = Hq / Hkv;
-    if (!me.plan(line, short_below, lane)) {
+    if (!me.plan(line, how, lane)) {
         zero_empty(pages, line, Hq, G, kHeads, D, out);
         me.step();
         return;
@@ -176,10 +179,16 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
         }
         Finder<kWhole> finder = {pages.table_of(p.entry), pages.page_size, len, t0 + warp, my_tiles, {}, {}};
         finder.start(lane);
-        const auto copy = [&](uint32_t stage, int j) { rows.copy(stage, t0 + warp + j * kWarps, finder.get(j, lane), lane); };   // the warp's j-th tile
+        // the warp's j-th tile: found, and which of its rows count left where the products look (eight places: more than there are stages)
+        const auto locate = [&](int j) __attribute__((always_inline)) {
+            const auto tile = rows.locate(t0 + warp + j * kWarps, finder.get(j, lane), lane);
+            if (lane == 0) sh_rows[warp][j & 7] = tile.rows_ok;
+            return tile;
+        };
+        static_assert(S::kStages < 8, "");
 #pragma unroll
         for (int s = 0; s < S::kStages; ++s) {
-            if (s < my_tiles) copy(ring + s * S::kStageBytes, s);
+            if (s < my_tiles) rows.copy(ring + s * S::kStageBytes, locate(s), lane);
             cp_async_commit();
         }
         // q^T as the B operand of every k-step: b0 = q[head g][16ks + 2tig, +1], b1 = same + 8
@@ -200,6 +209,9 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
 
         int at_stage = 0;
         for (int i = 0; i < my_tiles; ++i) {
+            typename Rows<D, kWhole>::Tile next = {};
+            const bool more = i + S::kStages < my_tiles;
+            if (more) next = locate(i + S::kStages);
             cp_async_wait<S::kStages - 1>();   // tile i has landed, the next ones are on their way
             __syncwarp();
             const uint32_t st = ring + at_stage * S::kStageBytes;
@@ -216,7 +228,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
                 ldmatrix_x4(st + k_row * S::kRowBytes + ((c ^ (k_row & 7)) << 4), a);
                 mma_bf16(s[ks & 3], a, qb[ks][0], qb[ks][1]);
             }
-            const unsigned rows_ok = *reinterpret_cast<const unsigned*>(st_p + 2 * S::kTileBytes + 64);
+            const unsigned rows_ok = sh_rows[warp][i & 7];
             float lc_lo = 0.f, lc_hi = 0.f;
             if (rows.count != nullptr) {
                 const int* cs = reinterpret_cast<const int*>(st_p + 2 * S::kTileBytes);
@@ -265,7 +277,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             }
             __syncwarp();
             // the stage just consumed takes the next tile
-            if (i + S::kStages < my_tiles) copy(st, i + S::kStages);
+            if (more) rows.copy(st, next, lane);
             cp_async_commit();
             at_stage = at_stage + 1 == S::kStages ? 0 : at_stage + 1;
         }
@@ -336,7 +348,7 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
         ready[dev & 63] = own_error(cudaFuncSetAttribute(paged_decode_mma<D, kWhole, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmemBytes));
     });
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
-    const Division part = divide(line, sms, [](int, int) { return Shape<D>::kBlocksPerSm; }, D);
+    const Division part = divide(line, sms, [](int, int) { return Shape<D>::kBlocksPerSm; }, D, Shape<D>::kBlocksPerSm > 1);
     const int c = part.cluster;
     const float scale = (a.scale == 0.f ? 1.f / sqrtf((float)a.d) : a.scale) * 1.4426950408889634f;
     cudaLaunchConfig_t cfg = {};
@@ -351,7 +363,7 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return own_error(cudaLaunchKernelEx(&cfg, paged_decode_mma<D, kWhole, kPair>, pages_of<const bf16>(a.cache), (const bf16*)a.q, a.Hq, a.Hkv, line, part.short_below,
+    return own_error(cudaLaunchKernelEx(&cfg, paged_decode_mma<D, kWhole, kPair>, pages_of<const bf16>(a.cache), (const bf16*)a.q, a.Hq, a.Hkv, line, part,
                                         scale, (bf16*)a.out, (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status));
 }
 
@@ -364,7 +376,7 @@ cudaError_t start(const PagedDecodeArgs& a, const Line& line, int dev, int sms, 
 
 }  // namespace
 
-Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d) {
+Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d, bool one_per_sm) {
     const int64_t units = (int64_t)line.entries * line.per_entry;
     // Up to 64 units: clusters of four, as many as find room at once (7/8 of the block slots: 64 of 4 x 74), and of those a multiple of the units
     // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.0
@@ -382,7 +394,7 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
         if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
         short_below = units <= 16 ? 0 : (unsigned)units * 512;
     }
-    return {c, short_below};
+    return {c, short_below, c == 1 && one_per_sm ? (unsigned)sms * kLongStretch : 0xffffffffu, sms};
 }
 
 }  // namespace pg

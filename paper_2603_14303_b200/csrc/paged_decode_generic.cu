@@ -37,7 +37,7 @@ __host__ __device__ constexpr int stages_of(int pitch) { return pitch <= 128 ? 3
 // kH: query heads of a unit.  kStages: of a warp's ring.  kChunks: a lane's chunks of columns.
 template <typename T, int kH, int kStages, int kChunks>
 __global__ void __launch_bounds__(kThreads, blocks_by_registers(kH))
-paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq, int Hkv, int d, Line line, unsigned short_below, float scale_log2,
+paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq, int Hkv, int d, Line line, const Division how, float scale_log2,
                      T* __restrict__ out, int32_t* __restrict__ tickets, float* __restrict__ part, int32_t* status) {
     constexpr int E = 16 / sizeof(T);
     extern __shared__ __align__(128) unsigned char smem[];
@@ -52,7 +52,7 @@ paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq
     me.set_up(sh_bar);
     in_stream_order();
     const int G = Hq / Hkv;
-    if (!me.plan(line, short_below, lane)) {
+    if (!me.plan(line, how, lane)) {
         zero_empty(pages, line, Hq, G, kH, d, out);
         me.step();
         return;
@@ -283,7 +283,7 @@ cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
     const Division part = divide(line, sms, [](int cluster, int d) {
         const int room = 228 * 1024 / (bytes_of<T, kH, kStages>(cluster, d) + 2560 + (kH > 4 ? 1024 : 0));
         return room < 1 ? 1 : room < blocks_by_registers(kH) ? room : blocks_by_registers(kH);
-    }, a.d);
+    }, a.d, false);
     const float scale = (a.scale == 0.f ? 1.f / sqrtf((float)a.d) : a.scale) * 1.4426950408889634f;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(line.parties * part.cluster);
@@ -297,7 +297,7 @@ cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return own_error(cudaLaunchKernelEx(&cfg, kernel, pages_of<const T>(a.cache), (const T*)a.q, a.Hq, a.Hkv, a.d, line, part.short_below, scale, (T*)a.out,
+    return own_error(cudaLaunchKernelEx(&cfg, kernel, pages_of<const T>(a.cache), (const T*)a.q, a.Hq, a.Hkv, a.d, line, part, scale, (T*)a.out,
                                         (int32_t*)a.ws, (float*)((char*)a.ws + kTicketBytes), a.status));
 }
 
