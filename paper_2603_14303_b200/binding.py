@@ -161,6 +161,7 @@ def _native():
         except ImportError as e:
             raise RuntimeError(f"_native_calls.so is missing or does not load ({e}): run "
                                "`python -m paper_2603_14303_b200.build`") from e
+        _native_calls.set_types(torch.int32, torch.float32)
         _native_module = _native_calls
     return _native_module
 
@@ -598,6 +599,10 @@ class PagedCache:
         for name, value in (("B", table.shape[0]), ("heads", heads), ("Hkv", heads if heads > 1 else th), ("table_heads", th), ("d", d), ("_dt", _dt(k)), ("_dev", dev),
                             ("_form", bytes(form))):
             object.__setattr__(self, name, value)
+        # what the native calls are told of a cache besides its addresses (heads: of a page, for an append; KV heads, for the others)
+        about = (k.dtype, self._dt, dev, self.B)
+        object.__setattr__(self, "_about_pages", (self._form, *about, heads, d))
+        object.__setattr__(self, "_about_heads", (self._form, *about, self.Hkv, d))
 
     def over(self, table: torch.Tensor) -> "PagedCache":
         """The same pages through another table: paged_select's choice, another batch."""
@@ -610,24 +615,7 @@ class PagedCache:
         return self.over(self.table.reshape(self.B * self.table_heads, 1, self.table.shape[2]))
 
     def _pointers(self):
-        return (self.k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(), _ptr(self.count), _ptr(self.k_min), _ptr(self.k_max),
-                self._form)
-
-
-def _lengths(t: torch.Tensor, n: int, dev: int, what: str):
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
-        raise ValueError(f"{what}: {n} contiguous int32 on the cache's device")
-
-
-def _heads_of_tokens(t: torch.Tensor, cache: PagedCache, what: str):
-    """Shape and element strides of rows [T, heads, d] of the cache's type (a stride is 0 where there is one entry)."""
-    if t.dim() != 3 or t.dtype is not cache.k.dtype or t.get_device() != cache._dev:
-        raise ValueError(f"{what}: [T, heads, d] of the cache's type, on its device")
-    T, H, d = t.shape
-    s0, s1, s2 = t.stride()
-    if d != cache.d or (s2 != 1 and T * H):
-        raise ValueError(f"{what}: [T, heads, {cache.d}], d contiguous")
-    return T, H, s0 if T > 1 else 0, s1 if H > 1 else 0
+        return self.k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(), _ptr(self.count), _ptr(self.k_min), _ptr(self.k_max)
 
 
 def _called(fn, dev: int, args):
@@ -642,80 +630,27 @@ def sc_paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, seq_len
                     inv_freq=None, positions=None, status=None, flags=0):
     """Raw sc_paged_append: rows k_new, v_new [T, Hkv, d] join the cache of their sequences (see the header).  ``inv_freq``
     (float32) turns the first 2 * len(inv_freq) columns of the keys, and of ``q`` [T, Hq, d] on its way to ``q_out``."""
-    dev, B = cache._dev, cache.B
-    T, Hkv, ks0, ks1 = rows = _heads_of_tokens(k_new, cache, "k_new")
-    if _heads_of_tokens(v_new, cache, "v_new") != rows:
-        raise ValueError("k_new and v_new: one shape and layout")
-    if Hkv != cache.heads:
-        raise ValueError("k_new and v_new: as many heads as a page of the cache")
-    _lengths(seq_off, B + 1, dev, "seq_off")
-    _lengths(cache_len, B, dev, "cache_len")
-    if seq_len is not None:
-        _lengths(seq_len, B, dev, "seq_len")
-    if len_out is not None:
-        _lengths(len_out, B, dev, "len_out")
-    if count_new is not None:
-        _lengths(count_new, T * Hkv, dev, "count_new")
-    if positions is not None:
-        _lengths(positions, T, dev, "positions")
-    Hq, qs0, qs1, qo0, qo1 = Hkv, 0, 0, 0, 0
-    if q is not None and q_out is not None:
-        Tq, Hq, qs0, qs1 = _heads_of_tokens(q, cache, "q")
-        To, Ho, qo0, qo1 = _heads_of_tokens(q_out, cache, "q_out")
-        if Tq != T or To != T or Ho != Hq:
-            raise ValueError("q and q_out: [T, Hq, d]")
-    elif q is not None or q_out is not None:
-        raise ValueError("q and q_out go together")
-    rot = 0
-    if inv_freq is not None:
-        if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous() or inv_freq.get_device() != dev:
-            raise ValueError("inv_freq: contiguous float32 on the cache's device")
-        rot = 2 * inv_freq.numel()
-    code = _called(_native().paged_append, dev, (
-        *cache._pointers(), k_new.data_ptr(), v_new.data_ptr(), ks0, ks1, _ptr(count_new), seq_off.data_ptr(), _ptr(seq_len),
-        cache_len.data_ptr(), _ptr(len_out), _ptr(q), _ptr(q_out), qs0, qs1, qo0, qo1, _ptr(inv_freq), rot, _ptr(positions), cache._dt, B, Hq,
-        Hkv, T, cache.d, int(flags), _ptr(status), _stream(k_new)))
+    code = _called(_native().paged_append, cache._dev, (
+        *cache._pointers(), *cache._about_pages, k_new, v_new, seq_off, cache_len, seq_len, count_new, len_out, q, q_out, inv_freq, positions,
+        status, int(flags), _stream(k_new)))
     if code != SC_OK:
         raise ScError("sc_paged_append", code)
 
 
-def _query(q: torch.Tensor, cache: PagedCache, what: str):
-    if q.dim() != 3 or q.dtype is not cache.k.dtype or not q.is_contiguous() or q.get_device() != cache._dev:
-        raise ValueError(f"{what}: contiguous [B, Hq, d] of the cache's type, on its device")
-    B, Hq, d = q.shape
-    if B != cache.B or d != cache.d:
-        raise ValueError(f"{what}: [{cache.B}, Hq, {cache.d}]")
-    return Hq
-
-
 def sc_paged_decode_attn(q, cache: PagedCache, lens, out, workspace, scale=0.0, status=None, flags=0):
     """Raw sc_paged_decode_attn: one decode step over a paged cache, q/out [B, Hq, d], lens int32 [B] or [B, table_heads]."""
-    dev, B = cache._dev, cache.B
-    Hq = _query(q, cache, "q")
-    if _query(out, cache, "out") != Hq:
-        raise ValueError("out: the shape of q")
-    _lengths(lens, B * cache.table_heads, dev, "lens")
-    if workspace.get_device() != dev:
-        raise ValueError("a workspace on the cache's device required")
-    code = _called(_native().paged_decode_attn, dev, (
-        *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, cache.Hkv, cache.d, lens.data_ptr(), float(scale), int(flags), out.data_ptr(),
-        workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(q)))
+    code = _called(_native().paged_decode_attn, cache._dev, (
+        *cache._pointers(), *cache._about_heads, q, lens, out, workspace, float(scale), status, int(flags), _stream(q)))
     if code != SC_OK:
         raise ScError("sc_paged_decode_attn", code)
 
 
 def sc_paged_select(q, cache: PagedCache, lens, keep, n_first, n_last, sel_table, sel_len, status=None):
     """Raw sc_paged_select: the ``keep`` pages of every (sequence, KV head) whose keys can score highest (see the header)."""
-    dev, B, Hkv = cache._dev, cache.B, cache.Hkv
-    Hq = _query(q, cache, "q")
     if cache.k_min is None:
         raise ValueError("a cache with k_min and k_max required")
-    _lengths(lens, B * cache.table_heads, dev, "lens")
-    _lengths(sel_table, B * Hkv * keep, dev, "sel_table")
-    _lengths(sel_len, B * Hkv, dev, "sel_len")
-    code = _called(_native().paged_select, dev, (
-        *cache._pointers(), q.data_ptr(), cache._dt, B, Hq, Hkv, cache.d, lens.data_ptr(), int(keep), int(n_first), int(n_last),
-        sel_table.data_ptr(), sel_len.data_ptr(), _ptr(status), _stream(q)))
+    code = _called(_native().paged_select, cache._dev, (
+        *cache._pointers(), *cache._about_heads, q, lens, int(keep), int(n_first), int(n_last), sel_table, sel_len, status, _stream(q)))
     if code != SC_OK:
         raise ScError("sc_paged_select", code)
 

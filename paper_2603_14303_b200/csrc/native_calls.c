@@ -144,48 +144,169 @@ static int cache_of(PyObject* const* a, sc_paged_cache* c) {
     c->k = ptr(a[0]); c->v = ptr(a[1]); c->table = ptr(a[2]); c->count = ptr(a[3]); c->k_min = ptr(a[4]); c->k_max = ptr(a[5]);
     return 1;
 }
-static int64_t i64(PyObject* o) { return PyLong_AsLongLong(o); }
+/* The calls on a paged cache take the tensors themselves and check them here: what a tensor is asked for from Python costs twice as
+ * much, and an append asks eleven of them (4 us of 7.5). */
+static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_data_ptr, *s_numel, *s_is_contiguous, *s_nbytes;
+static PyObject *t_int32, *t_float32;   /* the types, from set_types */
+
+static PyObject* set_types(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    if (!arity(n, 2, "set_types")) return NULL;
+    Py_INCREF(a[0]); Py_XSETREF(t_int32, a[0]);
+    Py_INCREF(a[1]); Py_XSETREF(t_float32, a[1]);
+    Py_RETURN_NONE;
+}
+static int refuse(const char* what, const char* why) {
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: %s", what, why);
+    return 0;
+}
+static int is_type(PyObject* t, PyObject* type) {
+    PyObject* x = PyObject_GetAttr(t, s_dtype);
+    Py_XDECREF(x);
+    return x != NULL && x == type;
+}
+static long long asked(PyObject* t, PyObject* method) {   /* of a method that gives an integer; -1 with an exception set */
+    PyObject* x = PyObject_CallMethodNoArgs(t, method);
+    if (!x) return -1;
+    const long long v = PyLong_AsLongLong(x);
+    Py_DECREF(x);
+    return v;
+}
+static void* address(PyObject* t) {                       /* None: NULL */
+    if (t == Py_None) return NULL;
+    PyObject* x = PyObject_CallMethodNoArgs(t, s_data_ptr);
+    if (!x) return NULL;
+    void* p = (void*)PyLong_AsUnsignedLongLong(x);
+    Py_DECREF(x);
+    return p;
+}
+static int three(PyObject* x, int64_t* v) {               /* a tuple of three integers; the reference is taken */
+    if (!x) return 0;
+    int ok = PyTuple_Check(x) && PyTuple_GET_SIZE(x) == 3;
+    for (int i = 0; ok && i < 3; ++i) {
+        v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(x, i));
+        if (v[i] == -1 && PyErr_Occurred()) ok = 0;
+    }
+    Py_DECREF(x);
+    return ok;
+}
+/* rows [n, heads, d]: sizes, element strides (0 where there is one entry) and address */
+typedef struct { int64_t n, heads, s0, s1; void* at; } rows3;
+static int rows_of(PyObject* t, PyObject* type, long dev, int64_t d, rows3* r, const char* what) {
+    int64_t size[3], step[3];
+    if (!is_type(t, type)) return refuse(what, "not of the cache's type");
+    if (asked(t, s_get_device) != dev) return refuse(what, "not on the cache's device");
+    if (!three(PyObject_GetAttr(t, s_shape), size) || !three(PyObject_CallMethodNoArgs(t, s_stride), step)) return refuse(what, "three axes expected");
+    if (size[2] != d || (step[2] != 1 && size[0] * size[1] > 0)) return refuse(what, "the last axis is the cache's head dimension, contiguous");
+    r->n = size[0]; r->heads = size[1];
+    r->s0 = size[0] > 1 ? step[0] : 0; r->s1 = size[1] > 1 ? step[1] : 0;
+    r->at = address(t);
+    return !PyErr_Occurred();
+}
+static int solid(const rows3* r, int64_t d) { return (r->n <= 1 || r->s0 == r->heads * d) && (r->heads <= 1 || r->s1 == d); }
+/* n contiguous values of a type; None gives NULL */
+static int list_of(PyObject* t, PyObject* type, long dev, int64_t n, void** at, const char* what) {
+    *at = NULL;
+    if (t == Py_None) return 1;
+    if (!is_type(t, type)) return refuse(what, "of another type");
+    if (asked(t, s_numel) != n) return refuse(what, "of another length");
+    if (asked(t, s_get_device) != dev) return refuse(what, "not on the cache's device");
+    PyObject* c = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+    Py_XDECREF(c);
+    if (c != Py_True) return refuse(what, "not contiguous");
+    *at = address(t);
+    return !PyErr_Occurred();
+}
+/* after the cache: its type's object and number, its device, tables, heads and head dimension */
+typedef struct { PyObject* type; sc_dtype dt; long dev; int32_t B, heads, d; } about;
+static int about_of(PyObject* const* a, about* c) {
+    c->type = a[0]; c->dt = (sc_dtype)i32(a[1]); c->dev = PyLong_AsLong(a[2]); c->B = i32(a[3]); c->heads = i32(a[4]); c->d = i32(a[5]);
+    return !PyErr_Occurred();
+}
 static PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     sc_paged_cache c;
     sc_paged_rows r;
+    about w;
+    rows3 k, v, q = {0, 0, 0, 0, NULL}, qo = {0, 0, 0, 0, NULL};
+    void *count, *off, *len, *have, *out, *freq, *pos;
     (void)self;
-    if (!arity(n, 34, "paged_append") || !cache_of(a, &c)) return NULL;
-    r.k = ptr(a[7]); r.v = ptr(a[8]); r.kv_token = i64(a[9]); r.kv_head = i64(a[10]); r.count = ptr(a[11]); r.seq_off = ptr(a[12]);
-    r.seq_len = ptr(a[13]); r.cache_len = ptr(a[14]); r.len_out = ptr(a[15]); r.q = ptr(a[16]); r.q_out = ptr(a[17]);
-    r.q_token = i64(a[18]); r.q_head = i64(a[19]); r.qo_token = i64(a[20]); r.qo_head = i64(a[21]); r.inv_freq = ptr(a[22]);
-    r.rot_dim = i32(a[23]); r.positions = ptr(a[24]);
-    const sc_dtype dt = (sc_dtype)i32(a[25]);
-    const int32_t B = i32(a[26]), Hq = i32(a[27]), Hkv = i32(a[28]), T = i32(a[29]), d = i32(a[30]);
-    const uint32_t flags = u32(a[31]);
-    void *status = ptr(a[32]), *stream = ptr(a[33]);
-    CALL(sc_paged_append(&c, &r, dt, B, Hq, Hkv, T, d, flags, status, stream));
+    if (!arity(n, 27, "paged_append") || !cache_of(a, &c) || !about_of(a + 7, &w)) return NULL;
+    PyObject* const* t = a + 13;   /* k_new, v_new, seq_off, cache_len, seq_len, count_new, len_out, q, q_out, inv_freq, positions */
+    if (!rows_of(t[0], w.type, w.dev, w.d, &k, "k_new") || !rows_of(t[1], w.type, w.dev, w.d, &v, "v_new")) return NULL;
+    if (k.n != v.n || k.heads != v.heads || k.s0 != v.s0 || k.s1 != v.s1) { refuse("k_new and v_new", "one shape and layout expected"); return NULL; }
+    if (k.heads != w.heads || k.n > INT32_MAX) { refuse("k_new", "as many heads as a page of the cache expected"); return NULL; }
+    if (t[2] == Py_None || t[3] == Py_None) { refuse("seq_off, cache_len", "expected"); return NULL; }
+    if (!list_of(t[2], t_int32, w.dev, (int64_t)w.B + 1, &off, "seq_off") || !list_of(t[3], t_int32, w.dev, w.B, &have, "cache_len") ||
+        !list_of(t[4], t_int32, w.dev, w.B, &len, "seq_len") || !list_of(t[5], t_int32, w.dev, k.n * k.heads, &count, "count_new") ||
+        !list_of(t[6], t_int32, w.dev, w.B, &out, "len_out") || !list_of(t[10], t_int32, w.dev, k.n, &pos, "positions")) return NULL;
+    if ((t[7] == Py_None) != (t[8] == Py_None)) { refuse("q and q_out", "both or neither expected"); return NULL; }
+    if (t[7] != Py_None) {
+        if (!rows_of(t[7], w.type, w.dev, w.d, &q, "q") || !rows_of(t[8], w.type, w.dev, w.d, &qo, "q_out")) return NULL;
+        if (q.n != k.n || qo.n != k.n || q.heads != qo.heads || q.heads > INT32_MAX) { refuse("q and q_out", "[T, Hq, d] expected"); return NULL; }
+    }
+    const long long freqs = t[9] == Py_None ? 0 : asked(t[9], s_numel);
+    if (PyErr_Occurred() || !list_of(t[9], t_float32, w.dev, freqs, &freq, "inv_freq")) return NULL;
+    if (freqs > INT32_MAX / 2) { refuse("inv_freq", "too long"); return NULL; }
+    r.k = k.at; r.v = v.at; r.kv_token = k.s0; r.kv_head = k.s1; r.count = count; r.seq_off = off; r.seq_len = len; r.cache_len = have; r.len_out = out;
+    r.q = q.at; r.q_out = qo.at; r.q_token = q.s0; r.q_head = q.s1; r.qo_token = qo.s0; r.qo_head = qo.s1;
+    r.inv_freq = freq; r.rot_dim = 2 * (int32_t)freqs; r.positions = pos;
+    const int32_t Hq = r.q != NULL ? (int32_t)q.heads : w.heads, T = (int32_t)k.n;
+    const uint32_t flags = u32(a[25]);
+    void *status = address(a[24]), *stream = ptr(a[26]);
+    CALL(sc_paged_append(&c, &r, w.dt, w.B, Hq, w.heads, T, w.d, flags, status, stream));
 }
-static PyObject* paged_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+static int query_of(PyObject* t, const about* w, rows3* q, const char* what) {
+    if (!rows_of(t, w->type, w->dev, w->d, q, what)) return 0;
+    if (q->n != w->B || q->heads > INT32_MAX || !solid(q, w->d)) return refuse(what, "contiguous [B, Hq, d] expected, B as the cache's tables");
+    return 1;
+}
+static PyObject* paged_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {   /* heads: the KV heads; then tables per sequence */
     sc_paged_cache c;
+    about w;
+    rows3 q, out;
+    void* lens;
     (void)self;
-    if (!arity(n, 21, "paged_decode_attn") || !cache_of(a, &c)) return NULL;
-    const void *q = ptr(a[7]), *lens = ptr(a[13]);
-    const sc_dtype dt = (sc_dtype)i32(a[8]);
-    const int32_t B = i32(a[9]), Hq = i32(a[10]), Hkv = i32(a[11]), d = i32(a[12]);
-    const float scale = f32(a[14]);
-    const uint32_t flags = u32(a[15]);
-    void *out = ptr(a[16]), *ws = ptr(a[17]), *status = ptr(a[19]), *stream = ptr(a[20]);
-    const size_t bytes = sz(a[18]);
-    CALL(sc_paged_decode_attn(&c, q, dt, B, Hq, Hkv, d, lens, scale, flags, out, ws, bytes, status, stream));
+    if (!arity(n, 21, "paged_decode_attn") || !cache_of(a, &c) || !about_of(a + 7, &w)) return NULL;
+    PyObject* const* t = a + 13;   /* q, lens, out, workspace, scale, status, flags, stream */
+    if (!query_of(t[0], &w, &q, "q") || !query_of(t[2], &w, &out, "out")) return NULL;
+    if (q.heads != out.heads) { refuse("out", "the shape of q expected"); return NULL; }
+    if (t[1] == Py_None || !list_of(t[1], t_int32, w.dev, (int64_t)w.B * c.table_heads, &lens, "lens")) { refuse("lens", "expected"); return NULL; }
+    if (asked(t[3], s_get_device) != w.dev) { refuse("workspace", "not on the cache's device"); return NULL; }
+    PyObject* bytes = PyObject_GetAttr(t[3], s_nbytes);
+    if (!bytes) return NULL;
+    const size_t have = sz(bytes);
+    Py_DECREF(bytes);
+    void *ws = address(t[3]), *status = address(t[5]), *stream = ptr(t[7]);
+    const float scale = f32(t[4]);
+    const uint32_t flags = u32(t[6]);
+    CALL(sc_paged_decode_attn(&c, q.at, w.dt, w.B, (int32_t)q.heads, w.heads, w.d, lens, scale, flags, out.at, ws, have, status, stream));
 }
 static PyObject* paged_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     sc_paged_cache c;
+    about w;
+    rows3 q;
+    void *lens, *table, *len;
     (void)self;
-    if (!arity(n, 21, "paged_select") || !cache_of(a, &c)) return NULL;
-    const void *q = ptr(a[7]), *lens = ptr(a[13]);
-    const sc_dtype dt = (sc_dtype)i32(a[8]);
-    const int32_t B = i32(a[9]), Hq = i32(a[10]), Hkv = i32(a[11]), d = i32(a[12]), keep = i32(a[14]), first = i32(a[15]), last = i32(a[16]);
-    void *table = ptr(a[17]), *len = ptr(a[18]), *status = ptr(a[19]), *stream = ptr(a[20]);
-    CALL(sc_paged_select(&c, q, dt, B, Hq, Hkv, d, lens, keep, first, last, table, len, status, stream));
+    if (!arity(n, 22, "paged_select") || !cache_of(a, &c) || !about_of(a + 7, &w)) return NULL;
+    PyObject* const* t = a + 13;   /* q, lens, keep, n_first, n_last, sel_table, sel_len, status, stream */
+    const int32_t keep = i32(t[2]), first = i32(t[3]), last = i32(t[4]);
+    if (PyErr_Occurred() || !query_of(t[0], &w, &q, "q")) return NULL;
+    if (t[1] == Py_None || t[5] == Py_None || t[6] == Py_None) { refuse("lens, sel_table, sel_len", "expected"); return NULL; }
+    if (!list_of(t[1], t_int32, w.dev, (int64_t)w.B * c.table_heads, &lens, "lens") ||
+        !list_of(t[5], t_int32, w.dev, (int64_t)w.B * w.heads * keep, &table, "sel_table") ||
+        !list_of(t[6], t_int32, w.dev, (int64_t)w.B * w.heads, &len, "sel_len")) return NULL;
+    void *status = address(t[7]), *stream = ptr(t[8]);
+    CALL(sc_paged_select(&c, q.at, w.dt, w.B, (int32_t)q.heads, w.heads, w.d, lens, keep, first, last, table, len, status, stream));
 }
 
 #define FN(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FN(chunk_sizes), FN(chunk), FN(compress), FN(decode_attn), FN(prefill_attn), FN(append), FN(append_layers),
-                                FN(paged_append), FN(paged_decode_attn), FN(paged_select), {NULL, NULL, 0, NULL}};
+                                FN(set_types), FN(paged_append), FN(paged_decode_attn), FN(paged_select), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
-PyMODINIT_FUNC PyInit__native_calls(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__native_calls(void) {
+    if (!(s_shape = PyUnicode_InternFromString("shape")) || !(s_stride = PyUnicode_InternFromString("stride")) ||
+        !(s_dtype = PyUnicode_InternFromString("dtype")) || !(s_get_device = PyUnicode_InternFromString("get_device")) ||
+        !(s_data_ptr = PyUnicode_InternFromString("data_ptr")) || !(s_numel = PyUnicode_InternFromString("numel")) ||
+        !(s_is_contiguous = PyUnicode_InternFromString("is_contiguous")) || !(s_nbytes = PyUnicode_InternFromString("nbytes"))) return NULL;
+    return PyModule_Create(&module);
+}

@@ -31,6 +31,18 @@ inline Pages<T> pages_of(const sc_paged_cache& c) {
 
 }  // namespace pg
 
+namespace pg {
+
+// The opt-ins of a kernel: its dynamic shared memory, and clusters beyond the portable size.
+template <typename K>
+inline cudaError_t opt_in(K kernel, int smem, bool wide) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && wide) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return own_error(e);
+}
+
+}  // namespace pg
+
 struct PagedDecodeArgs {
     sc_paged_cache cache;
     const void* q; sc_dtype dt; int32_t B, Hq, Hkv, d; const int32_t* lens;

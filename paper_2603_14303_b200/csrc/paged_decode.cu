@@ -345,7 +345,7 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
     static std::once_flag once[64];   // per device
     static cudaError_t ready[64];
     std::call_once(once[dev & 63], [dev] {
-        ready[dev & 63] = own_error(cudaFuncSetAttribute(paged_decode_mma<D, kWhole, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmemBytes));
+        ready[dev & 63] = opt_in(paged_decode_mma<D, kWhole, kPair>, Shape<D>::kSmemBytes, false);
     });
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
     const Division part = divide(line, sms, [](int, int) { return Shape<D>::kBlocksPerSm; }, D, Shape<D>::kBlocksPerSm > 1);

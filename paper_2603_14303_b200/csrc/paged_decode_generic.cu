@@ -275,7 +275,7 @@ cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
     static cudaError_t ready[64];
     const auto kernel = paged_decode_generic<T, kH, kStages, kChunks>;
     constexpr int kMost = kChunks * 32 * 16 / (int)sizeof(T) < kMaxD ? kChunks * 32 * 16 / (int)sizeof(T) : kMaxD;   // d
-    std::call_once(once[dev & 63], [&] { ready[dev & 63] = own_error(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_of<T, kH, kStages>(4, kMost))); });
+    std::call_once(once[dev & 63], [&] { ready[dev & 63] = opt_in(kernel, bytes_of<T, kH, kStages>(4, kMost), false); });
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
     Line line;
     line.lens = a.lens; line.entries = a.B * a.cache.table_heads; line.per_entry = a.Hkv / a.cache.table_heads * div_up(a.Hq / a.Hkv, kH);

@@ -573,9 +573,7 @@ cudaError_t start(const PagedSelectArgs& a, cudaStream_t st) {
     static std::once_flag once[64];   // per device
     static cudaError_t ready[64];
     std::call_once(once[dev & 63], [&] {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        ready[dev & 63] = own_error(e);
+        ready[dev & 63] = opt_in(kernel, kMaxSmem, true);
     });
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
     // As wide as leaves every block an SM, and 64 pages where the tables are full: 8 heads x 8192 pages in clusters of 16 27 us, of eight 28, of four 37; 32 heads
