@@ -18,7 +18,7 @@ constexpr int kMaxBlocks = 448;           // of a launch
 constexpr int kCluster = 4;               // blocks of a party, where it is a cluster
 constexpr int kMergeGroup = 8;            // partial sums read together
 constexpr unsigned kShortStretch = 64;    // tiles per block below which stretches are cut at the units' ends
-constexpr unsigned kLongStretch = 200;    // tiles per SM from which one block on each is better than two
+constexpr unsigned kLongUnit = 192;       // mean tiles of a unit from which one block on each SM is better than two
 constexpr int kLeast = 2;                 // tiles per warp that a stretch has at least
 constexpr int kMaxD = 256;
 __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * kHeads; }   // a partial sum: acc[8][d], m[8], l[8]

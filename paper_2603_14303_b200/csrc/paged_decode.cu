@@ -158,38 +158,70 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
     const int v_row = lm_r + ((lm_j >> 1) << 3), v_csel = lm_j & 1;    // V^T: (r0-7,c), (r0-7,c+1), (r8-15,c), (r8-15,c+1)
     const uint32_t ring = smem_u32(smem) + warp * (S::kStages * S::kStageBytes);
 
-    for (Place p = me.begin(line, lane);;) {
-        const int len = line.len(p.entry), nt = line.tiles(p.entry);
-        const int take = (int)min((unsigned)(nt - p.tile), me.left);
-        const Unit unit(pages, p.entry, p.unit, G, kHeads);
-        const int nh = unit.nh;
-        const int64_t hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
-        // this block's tiles of the segment, and this warp's: t0 + warp, t0 + warp + kWarps, ...
-        const int each = (take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, take), t1 = p.tile + min((me.crank + 1) * each, take);
-        const int my_tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
+    // Up to four query heads: the warps' sums have a place of their own (the receiving places of a block that stands for itself), so the next
+    // segment's first tiles are on their way while this one's warps meet (512 units of 24 tiles 29.2 us, 30.3 without).
+    constexpr bool kApart = kPair && D <= 128;
+    constexpr int kCols = kPair ? 4 : kHeads;            // columns of a warp's sums
+    static_assert(!kApart || kWarps * kCols * D * 4 <= 2 * recv_bytes(D, kHeads), "");
+    const bool apart = kApart && me.csize == 1;
+    float* slabs = reinterpret_cast<float*>(apart ? smem + S::kRingBytes : smem);
+
+    struct Segment {
+        Place p;
+        int nt, take, first, tiles, nh;   // the unit's tiles, the segment's; this warp's: first, first + kWarps, ...
+        int64_t hq0;
         Rows<D, kWhole> rows;
-        {
-            const int hp = pages.page_heads > 1 ? unit.h : 0;
-            rows.k = pages.k + hp * pages.head_stride; rows.v = pages.v + hp * pages.head_stride;
-            rows.count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
-            rows.count_page = (int64_t)pages.page_heads * pages.page_size;
-            rows.nowhere = q;
-            rows.page_stride = pages.page_stride; rows.row_stride = pages.row_stride;
-            rows.num_pages = pages.num_pages; rows.len = len; rows.status = status;
-        }
-        Finder<kWhole> finder = {pages.table_of(p.entry), pages.page_size, len, t0 + warp, my_tiles, {}, {}};
-        finder.start(lane);
-        // the warp's j-th tile: found, and which of its rows count left where the products look (eight places: more than there are stages)
-        const auto locate = [&](int j) __attribute__((always_inline)) {
-            const auto tile = rows.locate(t0 + warp + j * kWarps, finder.get(j, lane), lane);
-            if (lane == 0) sh_rows[warp][j & 7] = tile.rows_ok;
-            return tile;
-        };
-        static_assert(S::kStages < 8, "");
+        Finder<kWhole> finder;
+    };
+    const auto prepare = [&](const Place& p, unsigned left) {
+        Segment s;
+        const int len = line.len(p.entry);
+        s.p = p;
+        s.nt = line.tiles_of(len);
+        s.take = (int)min((unsigned)(s.nt - p.tile), left);
+        const Unit unit(pages, p.entry, p.unit, G, kHeads);
+        s.nh = unit.nh;
+        s.hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
+        const int each = (s.take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, s.take), t1 = p.tile + min((me.crank + 1) * each, s.take);
+        s.first = t0 + warp;
+        s.tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
+        const int hp = pages.page_heads > 1 ? unit.h : 0;
+        s.rows.k = pages.k + hp * pages.head_stride; s.rows.v = pages.v + hp * pages.head_stride;
+        s.rows.count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
+        s.rows.count_page = (int64_t)pages.page_heads * pages.page_size;
+        s.rows.nowhere = q;
+        s.rows.page_stride = pages.page_stride; s.rows.row_stride = pages.row_stride;
+        s.rows.num_pages = pages.num_pages; s.rows.len = len; s.rows.status = status;
+        s.finder = {pages.table_of(p.entry), pages.page_size, len, s.first, s.tiles, {}, {}};
+        s.finder.start(lane);
+        return s;
+    };
+    // the warp's j-th tile: found, and which of its rows count left where the products look (eight places: more than there are stages)
+    const auto locate = [&](Segment& s, int j) __attribute__((always_inline)) {
+        const auto tile = s.rows.locate(s.first + j * kWarps, s.finder.get(j, lane), lane);
+        if (lane == 0) sh_rows[warp][j & 7] = tile.rows_ok;
+        return tile;
+    };
+    static_assert(S::kStages < 8, "");
+    const auto fill = [&](Segment& s) __attribute__((always_inline)) {   // the whole ring
 #pragma unroll
-        for (int s = 0; s < S::kStages; ++s) {
-            if (s < my_tiles) rows.copy(ring + s * S::kStageBytes, locate(s), lane);
+        for (int i = 0; i < S::kStages; ++i) {
+            if (i < s.tiles) s.rows.copy(ring + i * S::kStageBytes, locate(s, i), lane);
             cp_async_commit();
+        }
+    };
+
+    Segment seg = prepare(me.begin(line, lane), me.left);
+    fill(seg);
+    for (;;) {
+        const int my_tiles = seg.tiles, nh = seg.nh;
+        const int64_t hq0 = seg.hq0;
+        const bool last = me.left == (unsigned)seg.take;
+        Segment then;
+        if (apart && !last) {            // (its pages are looked up meanwhile)
+            Place p = seg.p;
+            next_unit(line, p, seg.nt);
+            then = prepare(p, me.left - seg.take);
         }
         // q^T as the B operand of every k-step: b0 = q[head g][16ks + 2tig, +1], b1 = same + 8
         uint32_t qb[D / 16][2];
@@ -211,7 +243,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
         for (int i = 0; i < my_tiles; ++i) {
             typename Rows<D, kWhole>::Tile next = {};
             const bool more = i + S::kStages < my_tiles;
-            if (more) next = locate(i + S::kStages);
+            if (more) next = locate(seg, i + S::kStages);
             cp_async_wait<S::kStages - 1>();   // tile i has landed, the next ones are on their way
             __syncwarp();
             const uint32_t st = ring + at_stage * S::kStageBytes;
@@ -230,7 +262,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             }
             const unsigned rows_ok = sh_rows[warp][i & 7];
             float lc_lo = 0.f, lc_hi = 0.f;
-            if (rows.count != nullptr) {
+            if (seg.rows.count != nullptr) {
                 const int* cs = reinterpret_cast<const int*>(st_p + 2 * S::kTileBytes);
                 lc_lo = fast_log2((float)max(cs[g], 1));
                 lc_hi = fast_log2((float)max(cs[g + 8], 1));
@@ -277,11 +309,11 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             }
             __syncwarp();
             // the stage just consumed takes the next tile
-            if (more) rows.copy(st, next, lane);
+            if (more) seg.rows.copy(st, next, lane);
             cp_async_commit();
             at_stage = at_stage + 1 == S::kStages ? 0 : at_stage + 1;
         }
-        cp_async_wait<0>();
+        if (apart && !last) fill(then); else cp_async_wait<0>();
 
         // ---- the warps of this block meet (fixed order) ----
 #pragma unroll
@@ -293,32 +325,33 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             sh_m[warp][2 * tig] = m0; sh_m[warp][2 * tig + 1] = m1;
             sh_l[warp][2 * tig] = l0; sh_l[warp][2 * tig + 1] = l1;
         }
-        __syncthreads();   // every warp is done with its ring; reuse it as [warp][8 columns][D] fp32
+        __syncthreads();   // every warp is done with its ring: its place, or another one, takes [warp][columns][D] fp32
         float bm0 = -INFINITY, bm1 = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) { bm0 = fmaxf(bm0, sh_m[w][2 * tig]); bm1 = fmaxf(bm1, sh_m[w][2 * tig + 1]); }
         const float f0 = m0 == -INFINITY ? 0.f : dm::fast_exp2(m0 - bm0), f1 = m1 == -INFINITY ? 0.f : dm::fast_exp2(m1 - bm1);
-        float* slabs = reinterpret_cast<float*>(smem);
-        float* slab = slabs + warp * (kHeads * D);
+        float* slab = slabs + warp * (kCols * D);
 #pragma unroll
         for (int mt = 0; mt < D / 16; ++mt) {
             const int d0 = mt * 16 + g;
-            slab[(2 * tig) * D + d0] = o[mt][0] * f0;
-            slab[(2 * tig + 1) * D + d0] = o[mt][1] * f1;
-            slab[(2 * tig) * D + d0 + 8] = o[mt][2] * f0;
-            slab[(2 * tig + 1) * D + d0 + 8] = o[mt][3] * f1;
+            float v[4] = {o[mt][0] * f0, o[mt][1] * f1, o[mt][2] * f0, o[mt][3] * f1};
+            if (kPair) {   // the remainders' part (their columns' maxima are the same)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += __shfl_xor_sync(kFull, v[i], 2);
+                if (tig >= 2) continue;
+            }
+            slab[(2 * tig) * D + d0] = v[0];
+            slab[(2 * tig + 1) * D + d0] = v[1];
+            slab[(2 * tig) * D + d0 + 8] = v[2];
+            slab[(2 * tig + 1) * D + d0 + 8] = v[3];
         }
         __syncthreads();
         const auto block_sum = [&](int e4) {   // four columns of a head: e4 = head * D / 4 + column / 4
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float4 v = *reinterpret_cast<const float4*>(slabs + w * (kHeads * D) + e4 * 4);
+                const float4 v = *reinterpret_cast<const float4*>(slabs + w * (kCols * D) + e4 * 4);
                 acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-                if (kPair) {   // the remainders' part
-                    const float4 r = *reinterpret_cast<const float4*>(slabs + w * (kHeads * D) + 4 * D + e4 * 4);
-                    acc.x += r.x; acc.y += r.y; acc.z += r.z; acc.w += r.w;
-                }
             }
             return acc;
         };
@@ -330,11 +363,18 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             for (int w = 0; w < kWarps; ++w) bl += sh_m[w][hd] == -INFINITY ? 0.f : sh_l[w][hd] * dm::fast_exp2(sh_m[w][hd] - bm);
             return make_float2(bm, bl);
         };
-        joiner.join(me, p, nt, take, nh, D, out + hq0 * D, block_sum, block_ml);
-        me.left -= take;
-        if (me.left == 0) break;
-        next_unit(line, p, nt);
-        __syncthreads();   // the ring, sh_m and sh_l are written again
+        joiner.join(me, seg.p, seg.nt, seg.take, nh, D, out + hq0 * D, block_sum, block_ml);
+        if (last) break;
+        me.left -= seg.take;
+        __syncthreads();   // the sums' place, sh_m and sh_l are written again, and the ring where it is that place
+        if (apart) {
+            seg = then;
+        } else {
+            Place p = seg.p;
+            next_unit(line, p, seg.nt);
+            seg = prepare(p, me.left);
+            fill(seg);
+        }
     }
     zero_empty(pages, line, Hq, G, kHeads, D, out);
     joiner.leave(me);
@@ -354,7 +394,7 @@ cudaError_t start(const PagedDecodeArgs& a, Line line, int dev, int sms, cudaStr
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(line.parties * c);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = c > 1 ? Shape<D>::kSmemBytes : Shape<D>::kRingBytes;
+    cfg.dynamicSmemBytes = Shape<D>::kSmemBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -383,7 +423,9 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     // and 17, of 32 K 31.0 and 38.0, of 128 K 98 and 102; 4 units of 128 K with seven query heads 55 and 74; 16 units of 32 K 53 and 58.  Clusters
     // of eight: 1 K rows 7.8 and 9.8 (of four), but 8 K 15.7 and 13.2, because the next launch's clusters find room only when this one is gone.
     // From 17 units on each block stands for itself where the units are short: 32 units of 3 K rows 18.3 (clusters 21), of 25 K 81 and 81.
-    // More units: single blocks (128 units of 150 rows 12.8, in clusters of two 17.1; of 12 K rows 138 and 135; 512 of 1.5 K 73.5 and 76.2).
+    // More units: single blocks, two per SM (128 units of 150 rows 12.8, in clusters of two 17.1); where units are long one per SM, which reads
+    // fewer streams at a time (128 units of 6 K rows 71.8 and 73.9, of 12 K 124 and 128, of 16 K 166 and 175; but 512 of 1.5 K 73.0 and 69.7, 2048 of
+    // 400 rows 111 and 78; 128 units of 3 K and 512 of 3 K the same).
     const int c = units <= 64 ? kCluster : 1;
     int blocks = sms * blocks_of(c, d);
     if (blocks > kMaxBlocks) blocks = kMaxBlocks;
@@ -394,7 +436,7 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
         if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
         short_below = units <= 16 ? 0 : (unsigned)units * 512;
     }
-    return {c, short_below, c == 1 && one_per_sm ? (unsigned)sms * kLongStretch : 0xffffffffu, sms};
+    return {c, short_below, c == 1 && one_per_sm && units < 0x1000000 ? (unsigned)units * kLongUnit : 0xffffffffu, sms};
 }
 
 }  // namespace pg
