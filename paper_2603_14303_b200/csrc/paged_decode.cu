@@ -419,8 +419,8 @@ cudaError_t start(const PagedDecodeArgs& a, const Line& line, int dev, int sms, 
 Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d, bool one_per_sm) {
     const int64_t units = (int64_t)line.entries * line.per_entry;
     // Up to 64 units: clusters of four, as many as find room at once (7/8 of the block slots: 64 of 4 x 74), and of those a multiple of the units
-    // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.0
-    // and 17, of 32 K 31.0 and 38.0, of 128 K 98 and 102; 4 units of 128 K with seven query heads 55 and 74; 16 units of 32 K 53 and 58.  Clusters
+    // where that costs little, so that stretches of equal lengths end where units end.  us, against single blocks two per SM: 8 units of 8 K rows 13.2
+    // and 18.7, of 32 K 29.5 and 35.1, of 128 K 91 and 99; 4 units of 128 K with seven query heads 52 and 76; 32 units of 15 K 49.6 and 53.5.  Clusters
     // of eight: 1 K rows 7.8 and 9.8 (of four), but 8 K 15.7 and 13.2, because the next launch's clusters find room only when this one is gone.
     // From 17 units on each block stands for itself where the units are short: 32 units of 3 K rows 18.3 (clusters 21), of 25 K 81 and 81.
     // More units: single blocks, two per SM (128 units of 150 rows 12.8, in clusters of two 17.1); where units are long one per SM, which reads
@@ -433,6 +433,9 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     line.parties = blocks;
     if (c > 1) {
         line.parties = blocks * 7 / 8 / c;
+        int64_t most = (units * line.tiles_of(line.cap) + c * kWarps * kLeast - 1) / (c * kWarps * kLeast);   // what full tables could occupy
+        if (most < units) most = units;
+        if (most < line.parties) line.parties = (int)most;
         if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
         short_below = units <= 16 ? 0 : (unsigned)units * 512;
     }

@@ -425,9 +425,9 @@ select_pages(const Pages<const T> pages, const T* __restrict__ q, int Hq, int Hk
             }
         }
         // fp32: a piece's products in a row, the pieces, and the two halves of the columns, rounded to nearest.  bf16: the products are exact; a
-        // product's step adds 16 of them to the sum, in at least single precision but any order and rounding: 17 times 2^-22 at most.  (1.01:
-        // the norms' and sums' own rounding.  At the end: terms too small for fp32.)
-        const float unit = kMma ? (wide / 8 * 17) * 0x1p-22f : (kCols + pieces + 1) * 0x1p-24f;
+        // product's step adds 16 of them to the sum, in at least single precision but any order and rounding: what each addition drops is 2^-23
+        // of the sum of magnitudes at most.  (1.01: the norms' and sums' own rounding.  At the end: terms too small for fp32.)
+        const float unit = kMma ? (wide / 8 * 17) * 0x1p-23f : (kCols + pieces + 1) * 0x1p-24f;
         const float delta = unit * 1.01f * (sh_norm * __uint_as_float(largest)) + 0x1p-110f;
         uint32_t lo, hi;
         if (!(delta < INFINITY)) {
