@@ -554,7 +554,7 @@ def _step(t: torch.Tensor, dim: int) -> int:
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
-@dataclasses.dataclass(frozen=True)
+@dataclasses.dataclass(frozen=True, eq=False)
 class PagedCache:
     """One layer's keys and values in pages (``sc_paged_cache`` of the header).
 
@@ -578,12 +578,7 @@ class PagedCache:
         P, heads, ps, d = k.shape
         if d > 1 and (k.stride(3) != 1 or v.stride(3) != 1):
             raise ValueError("the head dimension of k and v must be contiguous")
-        if table.dim() not in (2, 3) or table.dtype != torch.int32:
-            raise ValueError("table: int32 [B, max_pages] or [B, heads, max_pages]")
-        th, W = (table.shape[1] if table.dim() == 3 else 1), table.shape[-1]
-        stride = table.stride(-2) if table.shape[-2] > 1 else table.stride(0) if table.shape[0] > 1 else W
-        if (W > 1 and table.stride(-1) != 1) or stride < W or (table.dim() == 3 and table.shape[0] > 1 and table.stride(0) != th * stride):
-            raise ValueError("table: rows evenly spaced, entries contiguous")
+        th, W, stride = self._table_shape(table)
         if self.count is not None and (self.count.dtype != torch.int32 or self.count.shape != (P, heads, ps) or not self.count.is_contiguous()):
             raise ValueError("count: contiguous int32 [pages, heads, page_size]")
         if (self.k_min is None) != (self.k_max is None):
@@ -596,17 +591,38 @@ class PagedCache:
             raise ValueError("the parts of a cache live on one device")
         form = _PagedCache(None, None, _step(k, 0), _step(k, 1), k.stride(2) if ps > 1 else d, P, ps, heads, None, stride, th, W, None, None,
                            None)
-        for name, value in (("B", table.shape[0]), ("heads", heads), ("Hkv", heads if heads > 1 else th), ("table_heads", th), ("d", d), ("_dt", _dt(k)), ("_dev", dev),
-                            ("_form", bytes(form))):
-            object.__setattr__(self, name, value)
-        # what the native calls are told of a cache besides its addresses (heads: of a page, for an append; KV heads, for the others)
-        about = (k.dtype, self._dt, dev, self.B)
-        object.__setattr__(self, "_about_pages", (self._form, *about, heads, d))
-        object.__setattr__(self, "_about_heads", (self._form, *about, self.Hkv, d))
+        self.__dict__.update(B=table.shape[0], heads=heads, Hkv=heads if heads > 1 else th, table_heads=th, d=d, _dt=_dt(k), _dev=dev)
+        self._tell(bytes(form))
+
+    @staticmethod
+    def _table_shape(table: torch.Tensor):
+        """Tables per sequence, entries per table, elements from one table to the next."""
+        if table.dim() not in (2, 3) or table.dtype != torch.int32:
+            raise ValueError("table: int32 [B, max_pages] or [B, heads, max_pages]")
+        shape, strides = table.shape, table.stride()
+        th, W = (shape[1] if len(shape) == 3 else 1), shape[-1]
+        stride = strides[-2] if shape[-2] > 1 else strides[0] if shape[0] > 1 else W
+        if (W > 1 and strides[-1] != 1) or stride < W or (len(shape) == 3 and shape[0] > 1 and strides[0] != th * stride):
+            raise ValueError("table: rows evenly spaced, entries contiguous")
+        return th, W, stride
 
     def over(self, table: torch.Tensor) -> "PagedCache":
         """The same pages through another table: paged_select's choice, another batch."""
-        return dataclasses.replace(self, table=table)
+        th, W, stride = self._table_shape(table)
+        if table.get_device() != self._dev:
+            raise ValueError("the parts of a cache live on one device")
+        form = _PagedCache.from_buffer_copy(self._form)
+        form.table_stride, form.table_heads, form.max_pages = stride, th, W
+        other = object.__new__(PagedCache)
+        other.__dict__.update(self.__dict__)
+        other.__dict__.update(table=table, B=table.shape[0], table_heads=th, Hkv=self.heads if self.heads > 1 else th)
+        other._tell(bytes(form))
+        return other
+
+    def _tell(self, form: bytes):
+        """What the native calls are told of a cache besides its addresses (heads: of a page, for an append; KV heads, for the others)."""
+        about = (self.k.dtype, self._dt, self._dev, self.B)
+        self.__dict__.update(_form=form, _about_pages=(form, *about, self.heads, self.d), _about_heads=(form, *about, self.Hkv, self.d))
 
     def one_head_sequences(self) -> "PagedCache":
         """A cache with tables and pages per head as B * Hkv sequences of one head each, the form in which it is appended to."""

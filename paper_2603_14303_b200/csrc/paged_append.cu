@@ -1,7 +1,7 @@
 // sc_paged_append: new rows of a ragged batch go into the pages of their sequences, keys and queries rotated on the way.
 //
-// One block serves one piece of one sequence: the new rows that fall into one page, for some of the heads (keys, values and
-// queries counted in one row).  So a page's bounds belong to one block per head, whose warps hold whole heads: smallest and
+// One block serves one piece of one sequence: the new rows that fall into one page (without bounds: into 64 rows of it), for some of the
+// heads (keys, values and queries counted in one row).  So a page's bounds belong to one block per head, whose warps hold whole heads: smallest and
 // largest key are taken in registers over the piece's rows and meet in a few shuffles; no atomics.  The host knows T and B only, from which
 // follow the most pieces there can be; which piece is a block's own it finds by counting all sequences' pieces.  (Places for two pieces more than
 // n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us.)
@@ -18,6 +18,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kSub = 16;          // rows whose sines and cosines are held at a time
 constexpr int kMaxHalf = 128;     // most pairs of a row
 constexpr int kGroupHeads = 32;   // most heads (keys, values, queries) per block
+constexpr int kCutRows = 64;
 
 template <typename T, int E> struct Vec;
 template <> struct Vec<__nv_bfloat16, 8> {
@@ -74,7 +75,8 @@ __device__ __forceinline__ float2 turn(int position, uint64_t step) {
     return make_float2(c, s);
 }
 
-struct Dims { int B, Hq, Hkv, T, d, group; };
+struct News { int first, n, have; bool fits; };   // a sequence's new rows: the first token, how many (-1: they break the rules), rows before, room
+struct Dims { int B, Hq, Hkv, T, d, group, cut, cuts; };   // cut: most rows of a piece, page_size or 64; cuts: pieces of a page
 
 // E: elements of a vector.  kUnits: units of a row (see below) where they fill a power of two of lanes and all columns are rotated, or none; 0: any.
 template <typename T, int E, bool kPairs, int kUnits>
@@ -83,6 +85,7 @@ __global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages
     // each four of neighbouring lanes lie side by side (as a plain list of pairs, read with 16-way bank conflicts, 35 K tokens x 48 heads took 265 us).
     __shared__ __align__(16) float sh_cos[kSub * kMaxHalf], sh_sin[kSub * kMaxHalf];
     __shared__ uint64_t sh_step[kMaxHalf];
+    __shared__ News sh_news;
     __shared__ int sh_seq, sh_piece, sh_sums[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = pages.page_size, B = dims.B, Hkv = dims.Hkv, d = dims.d;
@@ -91,41 +94,54 @@ __global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages
     __syncthreads();
     const int rot = rows.inv_freq != nullptr ? rows.rot_dim : 0, half = rot / 2;
     for (int i = tid; i < half; i += kThreads) sh_step[i] = turn_step(rows.inv_freq[i]);
-    int before = 0;                              // pieces of the sequences before these 256
-    for (int b0 = 0; b0 < B; b0 += kThreads) {
+    const auto news_of = [&](int b) {
+        const int o0 = rows.seq_off[b], o1 = rows.seq_off[b + 1], have = rows.cache_len[b];
+        const int n = rows.seq_len != nullptr ? rows.seq_len[b] : o1 - o0;
+        const bool valid = o0 >= 0 && o1 >= o0 && o1 <= dims.T && n >= 0 && n <= o1 - o0 && have >= 0;
+        return News{o0, valid ? n : -1, have, valid && (int64_t)have + n <= pages.cap()};
+    };
+    const auto tell = [&](int b, const News& w) {
+        if (!w.fits) set_status(status, w.n >= 0 ? SC_ERR_CAPACITY : SC_ERR_INVALID_ARG);
+        if (rows.len_out != nullptr) rows.len_out[b] = w.fits ? w.have + w.n : w.have;
+    };
+    if (blockIdx.y == 0 && B > kThreads)         // (fewer: in the loop below, by the first block)
+        for (int64_t b = (int64_t)blockIdx.x * kThreads + tid; b < B; b += (int64_t)gridDim.x * kThreads) tell((int)b, news_of((int)b));
+    // pieces of `cut` rows of every page, numbered along a sequence's rows
+    const unsigned cuts = dims.cuts;              // of a page
+    const auto piece_of = [&](unsigned row) {     // (a length near 2^31 and rows that do not fit: below 2^32)
+        const unsigned page = row / (unsigned)ps;
+        return cuts == 1 ? page : page * cuts + (row - page * ps) / (unsigned)dims.cut;
+    };
+    int before = 0;                              // pieces of the sequences so far
+    for (int b0 = 0; b0 < B && before <= (int)blockIdx.x; b0 += kThreads) {
         const int b = b0 + tid;
         int pieces = 0;
+        News w = {0, 0, 0, false};
         if (b < B) {
-            const int o0 = rows.seq_off[b], o1 = rows.seq_off[b + 1], have = rows.cache_len[b];
-            const int n = rows.seq_len != nullptr ? rows.seq_len[b] : o1 - o0;
-            const bool placed = o0 >= 0 && o1 >= o0 && o1 <= dims.T, valid = placed && n >= 0 && n <= o1 - o0 && have >= 0;
-            const bool fits = valid && (int64_t)have + n <= pages.cap();
-            if (valid && n > 0) pieces = (have % ps + n - 1) / ps + 1;
-            if (blockIdx.y == 0 && b % gridDim.x == blockIdx.x) {
-                if (!fits) set_status(status, valid ? SC_ERR_CAPACITY : SC_ERR_INVALID_ARG);
-                if (rows.len_out != nullptr) rows.len_out[b] = fits ? have + n : have;
-            }
+            w = news_of(b);
+            if (B <= kThreads && blockIdx.x == 0 && blockIdx.y == 0) tell(b, w);
+            if (w.n > 0) pieces = (int)(piece_of((unsigned)w.have + w.n - 1) - piece_of(w.have)) + 1;
         }
         const int upto = warp_scan_add(pieces, lane);
         if (lane == 31) sh_sums[warp] = upto;
         __syncthreads();
         int first = before + upto - pieces;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            first += w < warp ? sh_sums[w] : 0;
-            before += sh_sums[w];
+        for (int i = 0; i < kWarps; ++i) {
+            first += i < warp ? sh_sums[i] : 0;
+            before += sh_sums[i];
         }
-        if ((unsigned)((int)blockIdx.x - first) < (unsigned)pieces) { sh_seq = b; sh_piece = (int)blockIdx.x - first; }
+        if ((unsigned)((int)blockIdx.x - first) < (unsigned)pieces) { sh_seq = b; sh_piece = (int)blockIdx.x - first; sh_news = w; }
         __syncthreads();
     }
-    const int b = sh_seq, piece = sh_piece;
+    const int b = sh_seq;
     if (b < 0) return;
-    const int o0 = rows.seq_off[b], have = rows.cache_len[b];
-    const int n = rows.seq_len != nullptr ? rows.seq_len[b] : rows.seq_off[b + 1] - o0;
-    const bool fits = (int64_t)have + n <= pages.cap();
-    // the piece: rows [r0, r1) of the sequence (64 bits: a length near 2^31 with rows that do not fit)
-    const int64_t slot = have / ps + (int64_t)piece, p0 = slot * ps;
-    const int64_t r0 = p0 > have ? p0 : have, r1 = min(p0 + ps, (int64_t)have + n);
+    const int o0 = sh_news.first, have = sh_news.have, n = sh_news.n;
+    const bool fits = sh_news.fits;
+    // the piece: rows [r0, r1) of the sequence, of the page whose first row is p0 (64 bits: a length near 2^31 with rows that do not fit)
+    const unsigned piece = piece_of(have) + sh_piece, slot = cuts == 1 ? piece : piece / cuts;
+    const int64_t p0 = (int64_t)slot * ps, c0 = p0 + (int64_t)(piece - slot * cuts) * dims.cut;
+    const int64_t r0 = c0 > have ? c0 : have, r1 = min(min(c0 + dims.cut, p0 + ps), (int64_t)have + n);
     if (r0 >= r1) return;
     const int nr = (int)(r1 - r0), in_page = (int)(r0 - p0), tok0 = o0 + (int)(r0 - have);
     int id = -1;
@@ -309,12 +325,15 @@ cudaError_t run(const PagedAppendArgs& a, cudaStream_t st) {
     int dev = 0, sms = 148;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    int64_t blocks = a.T / a.cache.page_size + 2ll * a.B;   // n rows touch n / page_size + 2 pages at most, and no more than n
+    // A page's bounds belong to one block; without them long pages are shared out.  n rows touch n / page_size + 2 pages at most, n / cut + 2 + 1 per
+    // page's end pieces of them, and no more than n.
+    const int cut = a.cache.k_min != nullptr || a.cache.page_size < kCutRows ? a.cache.page_size : kCutRows;
+    int64_t blocks = a.T / cut + 2ll * a.B + (cut < a.cache.page_size ? a.T / a.cache.page_size + 2ll * a.B : 0);
     if (blocks > a.T) blocks = a.T > 0 ? a.T : 1;
-    const int64_t pieces = blocks < a.T / a.cache.page_size + a.B ? blocks : a.T / a.cache.page_size + a.B;   // about
+    const int64_t pieces = blocks < a.T / cut + a.B ? blocks : a.T / cut + a.B;   // about
     int64_t groups = div_up(heads, kGroupHeads);
     if (groups * pieces < 2 * sms) groups = 2 * sms / pieces < div_up(heads, 8) ? 2 * sms / pieces : div_up(heads, 8);
-    const Dims dims = {a.B, a.Hq, a.Hkv, a.T, a.d, div_up(heads, groups)};
+    const Dims dims = {a.B, a.Hq, a.Hkv, a.T, a.d, div_up(heads, groups), cut, div_up(a.cache.page_size, cut)};
     if (blocks > 0x7fffffff || groups > 65535) return cudaErrorInvalidConfiguration;
     const Pages<T> pages = pages_of<T>(a.cache);
     const dim3 grid((unsigned)blocks, (unsigned)groups);

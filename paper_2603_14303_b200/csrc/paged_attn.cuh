@@ -60,7 +60,7 @@ struct Place {              // a position on the line
 // Length of the line.  All lanes of a warp call it.
 __device__ __forceinline__ unsigned total_of(const Line& line, int lane) {
     unsigned sum = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int e = lane; e < line.entries; e += 32) sum += line.tiles(e);
     return __reduce_add_sync(kFull, sum) * line.per_entry;
 }

@@ -104,12 +104,18 @@ def test_page_sizes(ps, bounds):
     _run(BF, 2, 2, 64, ps, [0, 1, 15, 16, 300], [33, 1, 2, 16, 270], "nhd", bounds=bounds)
 
 
+@pytest.mark.parametrize("ps", [63, 64, 65, 100, 128, 1000, 100000])
+def test_long_pages_are_shared_out(ps):
+    """Without bounds a page's rows may be several blocks' work."""
+    _run(BF, 2, 4, 64, ps, [0, 1, 64, 150, 63], [300, 65, 128, 1, 2], "nhd", gap=3)
+
+
 @pytest.mark.parametrize("Hkv,Hq", [(1, 1), (1, 32), (8, 8), (3, 21), (32, 64), (70, 70)])
 def test_heads(Hkv, Hq):
     _run(BF, Hkv, Hq, 32, 16, [2, 30], [1, 20], bounds=True)
 
 
-@pytest.mark.parametrize("B", [1, 2, 300, 700])
+@pytest.mark.parametrize("B", [1, 2, 255, 256, 257, 700])
 def test_single_tokens(B):
     _run(BF, 2, 4, 128, 16, [(7 * b) % 50 for b in range(B)], [1] * B, "nhd", bounds=True)
 

@@ -93,6 +93,18 @@ def test_head_sizes(dtype, d):
     _check(dtype, 3, 2, 3, d, 16, [200, 1, 90], count=True)
 
 
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("G", [4, 8])
+def test_generic_kernels_of_the_other_head_sizes(G, d):
+    _check(BF, 3, 2, G, d, 16, [700, 15, 0], "nhd", flags=binding.SC_FLAG_GENERIC)
+    _check(BF, 1, 2, G, d, 24, [5000], flags=binding.SC_FLAG_GENERIC)
+
+
+@pytest.mark.parametrize("B,n", [(1500, 20), (2200, 3)])
+def test_more_sequences_than_blocks(B, n):
+    _check(BF, B, 1, 4, 64, 16, [(b * 7) % n for b in range(B)])
+
+
 @pytest.mark.parametrize("G,d", [(4, 64), (8, 64), (16, 64), (4, 256), (8, 256), (5, 256)])
 @pytest.mark.parametrize("ps", [16, 24])
 def test_head_sizes_and_groups(G, d, ps):

@@ -68,6 +68,17 @@ def test_many_pages(pages):
     _random(F32, 2, 1, 2, 32, 4, [pages * 4, pages * 2], 17)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_widest_tables(dtype):
+    """As many pages as a call takes, more of them kept than are ranked in shared memory; few of them in use under wide tables."""
+    W = binding.SC_SELECT_MAX_PAGES
+    for n, keep in ((W * 2 - 1, 3000), (40000, 17), (300, 100)):
+        table, mn, mx = _pages(dtype, 1, 1, 16, 2, [[n]])
+        table = torch.cat([table, torch.full((1, 1, W - table.shape[2]), -1, dtype=torch.int32)], 2) if table.shape[2] < W else table[:, :, :W].contiguous()
+        q = torch.randn((1, 2, 16), generator=torch.Generator().manual_seed(1)).to(dtype)
+        _check(dtype, q, table, mn, mx, torch.tensor([[n]], dtype=torch.int32), 2, keep, 1, 2)
+
+
 def test_tables_per_head():
     _random(BF, 2, 3, 4, 128, 16, [(50, 700, 0), (1000, 333, 16)], 9, own_pages=True)
     _random(F32, 2, 3, 4, 128, 16, [(50, 700, 0), (1000, 333, 16)], 9)
