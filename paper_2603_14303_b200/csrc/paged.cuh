@@ -13,6 +13,7 @@ struct Pages {
     const int32_t* table;
     int64_t page_stride, head_stride, row_stride, table_stride;
     int num_pages, page_size, page_heads, table_heads, max_pages;
+    int page_bits;                // page_size = 2^page_bits, or -1
 
     __host__ __device__ int cap() const { return max_pages * page_size; }
     __device__ const int32_t* table_of(int entry) const { return table + entry * table_stride; }   // entry = b * table_heads + ht
@@ -26,6 +27,9 @@ inline Pages<T> pages_of(const sc_paged_cache& c) {
     p.table = c.table; p.page_stride = c.page_stride; p.head_stride = c.head_stride; p.row_stride = c.row_stride;
     p.table_stride = c.table_stride; p.num_pages = c.num_pages; p.page_size = c.page_size; p.page_heads = c.page_heads;
     p.table_heads = c.table_heads; p.max_pages = c.max_pages;
+    p.page_bits = -1;
+    for (int i = 0; i < 31; ++i)
+        if (c.page_size == 1 << i) p.page_bits = i;
     return p;
 }
 

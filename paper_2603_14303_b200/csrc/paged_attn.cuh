@@ -15,7 +15,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;                 // rows a warp takes at a time
 constexpr int kHeads = 8;                 // most query heads of a unit
 constexpr int kMaxBlocks = 448;           // of a launch
-constexpr int kCluster = 4;               // blocks of a party, where it is a cluster
+constexpr int kCluster = 8;               // most blocks of a party
 constexpr int kMergeGroup = 8;            // partial sums read together
 constexpr unsigned kShortStretch = 64;    // tiles per block below which stretches are cut at the units' ends
 constexpr unsigned kLongUnit = 192;       // mean tiles of a unit from which one block on each SM is better than two
@@ -45,10 +45,10 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 constexpr size_t kTicketBytes = 4096;
 struct Line {
     const int32_t* lens;
-    int entries, per_entry, cap, tile, parties;   // per_entry: units of an entry
+    int entries, per_entry, cap, parties;   // per_entry: units of an entry
 
     __device__ __forceinline__ int len(int e) const { return max(min(lens[e], cap), 0); }
-    __host__ __device__ __forceinline__ int tiles_of(int n) const { return n > 0 ? (int)((unsigned)(n - 1) / (unsigned)tile) + 1 : 0; }   // (n may be 2^31 - 1)
+    __host__ __device__ __forceinline__ int tiles_of(int n) const { return n > 0 ? (n - 1) / kTile + 1 : 0; }   // (n may be 2^31 - 1)
     __device__ __forceinline__ int tiles(int e) const { return tiles_of(len(e)); }
     // Positions on the line are 32-bit numbers, which the entry point sees to: several divisions lie on the way to the first load.
 };
@@ -57,11 +57,19 @@ struct Place {              // a position on the line
     unsigned at;            // of the unit's first tile
 };
 
+// The tiles of up to kCutEntries entries, entry lane + 32 i in t[i], which both steps below look at.
+constexpr int kCutEntries = 128;
+struct Few { unsigned t[kCutEntries / 32]; };
 // Length of the line.  All lanes of a warp call it.
-__device__ __forceinline__ unsigned total_of(const Line& line, int lane) {
+__device__ __forceinline__ unsigned total_of(const Line& line, int lane, Few& few) {
     unsigned sum = 0;
+#pragma unroll
+    for (int i = 0; i < kCutEntries / 32; ++i) {
+        few.t[i] = lane + 32 * i < line.entries ? line.tiles(lane + 32 * i) : 0;
+        sum += few.t[i];
+    }
 #pragma unroll 8
-    for (int e = lane; e < line.entries; e += 32) sum += line.tiles(e);
+    for (int e = kCutEntries + lane; e < line.entries; e += 32) sum += line.tiles(e);
     return __reduce_add_sync(kFull, sum) * line.per_entry;
 }
 
@@ -89,13 +97,11 @@ __device__ __forceinline__ Place place_of(const Line& line, unsigned at, int lan
 // A line whose stretches would be short is cut at the units' ends instead, so that a party has one segment and fills its pipeline once:
 // every unit in as many equal parts as have `longest` tiles at most, `longest` the least for which there are parties enough (at most an
 // eighth over it).  For at most kCutEntries entries and no more units than parties.  All lanes of a warp call it.
-constexpr int kCutEntries = 128;
 struct Part { int entry, unit, tile, take, index, parts; };   // take 0: this party has none
-__device__ __forceinline__ Part part_of(const Line& line, unsigned longest, unsigned party, int lane) {
+__device__ __forceinline__ Part part_of(const Line& line, const Few& few, unsigned longest, unsigned party, int lane) {
     constexpr int kN = kCutEntries / 32;
-    unsigned t[kN], c[kN], sum;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) t[i] = lane + 32 * i < line.entries ? line.tiles(lane + 32 * i) : 0;
+    const auto& t = few.t;
+    unsigned c[kN], sum;
     for (;; longest += longest / 8 + 1) {
         sum = 0;
 #pragma unroll
@@ -175,7 +181,8 @@ struct Party {
     }
     // Whether the block has anything to do.
     __device__ __forceinline__ bool plan(Line& line, const Division& how, int lane) {
-        const unsigned total = total_of(line, lane);
+        Few few;
+        const unsigned total = total_of(line, lane, few);
         if (total < how.short_below) {
             step();
             csize = 1; crank = 0; party = blockIdx.x;
@@ -186,7 +193,7 @@ struct Party {
         cut = stretch < kShortStretch * csize && line.entries <= kCutEntries && line.entries * line.per_entry <= line.parties;
         from = 0;
         if (cut) {
-            own = part_of(line, stretch, party, lane);
+            own = part_of(line, few, stretch, party, lane);
             left = own.take;
         } else {
             from = min((uint64_t)party * stretch, (uint64_t)total);
@@ -204,10 +211,15 @@ struct Unit {
     int b, h, g0, nh;            // sequence, KV head, first query head of the group within it, query heads
     template <typename T>
     __device__ __forceinline__ Unit(const Pages<T>& pages, int entry, int unit, int G, int group) {
-        const int groups = (G + group - 1) / group;
-        b = entry / pages.table_heads;
-        h = pages.table_heads > 1 ? entry - b * pages.table_heads : unit / groups;
-        g0 = unit % groups * group;
+        b = pages.table_heads > 1 ? entry / pages.table_heads : entry;
+        int rest = 0;
+        if (G > group) {
+            const int groups = (G + group - 1) / group;
+            rest = unit % groups;
+            unit /= groups;
+        }
+        h = pages.table_heads > 1 ? entry - b * pages.table_heads : unit;
+        g0 = rest * group;
         nh = min(group, G - g0);
     }
 };
@@ -242,7 +254,7 @@ template <bool kWhole>
 struct Finder {
     static constexpr int kBatch = kWhole ? 32 : 2;
     const int32_t* table;
-    int page_size, len, first, n;     // n: the warp's tiles
+    int page_size, page_bits, len, first, n;     // page_bits: of a page_size that is a power of two, else -1; n: the warp's tiles
     int2 batch, next;
 
     __device__ __forceinline__ int2 look_up(int j0, int lane) const {
@@ -251,7 +263,7 @@ struct Finder {
         if (j >= n) return at;
         const int row = (first + j * kWarps) * kTile + (kWhole ? 0 : lane & 15);
         if (row < len) {
-            const int slot = row / page_size;
+            const int slot = page_bits >= 0 ? row >> page_bits : row / page_size;
             at = make_int2(table[slot], row - slot * page_size);
         }
         return at;

@@ -192,7 +192,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
         s.rows.nowhere = q;
         s.rows.page_stride = pages.page_stride; s.rows.row_stride = pages.row_stride;
         s.rows.num_pages = pages.num_pages; s.rows.len = len; s.rows.status = status;
-        s.finder = {pages.table_of(p.entry), pages.page_size, len, s.first, s.tiles, {}, {}};
+        s.finder = {pages.table_of(p.entry), pages.page_size, pages.page_bits, len, s.first, s.tiles, {}, {}};
         s.finder.start(lane);
         return s;
     };
@@ -426,7 +426,9 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     // More units: single blocks, two per SM (128 units of 150 rows 12.8, in clusters of two 17.1); where units are long one per SM, which reads
     // fewer streams at a time (128 units of 6 K rows 71.8 and 73.9, of 12 K 124 and 128, of 16 K 166 and 175; but 512 of 1.5 K 73.0 and 69.7, 2048 of
     // 400 rows 111 and 78; 128 units of 3 K and 512 of 3 K the same).
-    const int c = units <= 64 ? kCluster : 1;
+    // Tables of no more than 2.5 K rows, up to 16 units: clusters of eight, one per unit (8 units of 2 K rows 8.1 and 8.9, of 0.5 K 5.9 and 7.0).
+    const bool small = units <= 16 && line.tiles_of(line.cap) <= 5 * 8 * kWarps;
+    const int c = small ? 8 : units <= 64 ? 4 : 1;
     int blocks = sms * blocks_of(c, d);
     if (blocks > kMaxBlocks) blocks = kMaxBlocks;
     unsigned short_below = 0;
@@ -455,7 +457,7 @@ cudaError_t launch_paged_decode_mma(const PagedDecodeArgs& a, cudaStream_t st) {
     pg::Line line;
     line.lens = a.lens; line.entries = a.B * a.cache.table_heads;
     line.per_entry = a.Hkv / a.cache.table_heads * div_up(a.Hq / a.Hkv, pg::kHeads);
-    line.cap = a.cache.max_pages * a.cache.page_size; line.tile = pg::kTile;
+    line.cap = a.cache.max_pages * a.cache.page_size;
     const cudaError_t e = a.d == 64 ? pg::start<64>(a, line, dev, sms, st) : a.d == 128 ? pg::start<128>(a, line, dev, sms, st) : pg::start<256>(a, line, dev, sms, st);
     if (e == cudaSuccess) note_launches(1);
     return e;

@@ -76,7 +76,7 @@ paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq
         const T* kh = pages.k + hp * pages.head_stride;
         const T* vh = pages.v + hp * pages.head_stride;
         const int32_t* count = pages.count != nullptr ? pages.count + (int64_t)hp * pages.page_size : nullptr;
-        Finder<false> finder = {pages.table_of(p.entry), pages.page_size, len, t0 + warp, my_tiles, {}, {}};
+        Finder<false> finder = {pages.table_of(p.entry), pages.page_size, pages.page_bits, len, t0 + warp, my_tiles, {}, {}};
         finder.start(lane);
         const auto copy = [&](int stage_no, int j) {
             const uint32_t stage = ring + stage_no * stage_size;
@@ -279,7 +279,7 @@ cudaError_t start(const PagedDecodeArgs& a, cudaStream_t st) {
     if (ready[dev & 63] != cudaSuccess) return ready[dev & 63];
     Line line;
     line.lens = a.lens; line.entries = a.B * a.cache.table_heads; line.per_entry = a.Hkv / a.cache.table_heads * div_up(a.Hq / a.Hkv, kH);
-    line.cap = a.cache.max_pages * a.cache.page_size; line.tile = kTile;
+    line.cap = a.cache.max_pages * a.cache.page_size;
     const Division part = divide(line, sms, [](int cluster, int d) {
         const int room = 228 * 1024 / (bytes_of<T, kH, kStages>(cluster, d) + 2560 + (kH > 4 ? 1024 : 0));
         return room < 1 ? 1 : room < blocks_by_registers(kH) ? room : blocks_by_registers(kH);
