@@ -2,7 +2,7 @@
 //
 // One block serves one piece of one sequence: the new rows that fall into one page (without bounds: into 64 rows of it), for some of the
 // heads (keys, values and queries counted in one row).  So a page's bounds belong to one block per head, whose warps hold whole heads: smallest and
-// largest key are taken in registers over the piece's rows and meet in a few shuffles; no atomics.  The host knows T and B only, from which
+// largest key are taken in registers over the piece's rows, as stored and two at a time in bf16, and meet in a few shuffles; no atomics.  The host knows T and B only, from which
 // follow the most pieces there can be; which piece is a block's own it finds by counting all sequences' pieces.  (Places for two pieces more than
 // n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us.)
 // Sines and cosines of a piece's rows are taken once per block, 16 rows at a time, and shared by its heads.
@@ -19,6 +19,12 @@ constexpr int kSub = 16;          // rows whose sines and cosines are held at a 
 constexpr int kMaxHalf = 128;     // most pairs of a row
 constexpr int kGroupHeads = 32;   // most heads (keys, values, queries) per block
 constexpr int kCutRows = 64;
+
+// The smaller and the larger; not a number where one is not (a page with such a key must not lose it).
+__device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
+__device__ __forceinline__ uint32_t min_nan2(uint32_t a, uint32_t b) { uint32_t y; asm("min.NaN.bf16x2 %0, %1, %2;\n" : "=r"(y) : "r"(a), "r"(b)); return y; }
+__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) { uint32_t y; asm("max.NaN.bf16x2 %0, %1, %2;\n" : "=r"(y) : "r"(a), "r"(b)); return y; }
 
 template <typename T, int E> struct Vec;
 template <> struct Vec<__nv_bfloat16, 8> {
@@ -39,6 +45,14 @@ template <> struct Vec<__nv_bfloat16, 8> {
         }
         w = make_uint4(a[0], a[1], a[2], a[3]);
     }
+    __device__ __forceinline__ void fill(float x) { const float v[8] = {x, x, x, x, x, x, x, x}; set(v); }
+    __device__ __forceinline__ void lower(const Vec& o) { w = make_uint4(min_nan2(w.x, o.w.x), min_nan2(w.y, o.w.y), min_nan2(w.z, o.w.z), min_nan2(w.w, o.w.w)); }
+    __device__ __forceinline__ void raise(const Vec& o) { w = make_uint4(max_nan2(w.x, o.w.x), max_nan2(w.y, o.w.y), max_nan2(w.z, o.w.z), max_nan2(w.w, o.w.w)); }
+    __device__ __forceinline__ Vec from(int o) const {
+        Vec v;
+        v.w = make_uint4(__shfl_xor_sync(kFull, w.x, o), __shfl_xor_sync(kFull, w.y, o), __shfl_xor_sync(kFull, w.z, o), __shfl_xor_sync(kFull, w.w, o));
+        return v;
+    }
 };
 template <> struct Vec<float, 4> {
     float4 w;
@@ -46,6 +60,14 @@ template <> struct Vec<float, 4> {
     __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = w; }
     __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w; }
     __device__ __forceinline__ void set(const float (&x)[4]) { w = make_float4(x[0], x[1], x[2], x[3]); }
+    __device__ __forceinline__ void fill(float x) { w = make_float4(x, x, x, x); }
+    __device__ __forceinline__ void lower(const Vec& o) { w = make_float4(min_nan(w.x, o.w.x), min_nan(w.y, o.w.y), min_nan(w.z, o.w.z), min_nan(w.w, o.w.w)); }
+    __device__ __forceinline__ void raise(const Vec& o) { w = make_float4(max_nan(w.x, o.w.x), max_nan(w.y, o.w.y), max_nan(w.z, o.w.z), max_nan(w.w, o.w.w)); }
+    __device__ __forceinline__ Vec from(int o) const {
+        Vec v;
+        v.w = make_float4(__shfl_xor_sync(kFull, w.x, o), __shfl_xor_sync(kFull, w.y, o), __shfl_xor_sync(kFull, w.z, o), __shfl_xor_sync(kFull, w.w, o));
+        return v;
+    }
 };
 template <typename T> struct Vec<T, 1> {
     T w;
@@ -53,11 +75,11 @@ template <typename T> struct Vec<T, 1> {
     __device__ __forceinline__ void store(T* p) const { *p = w; }
     __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = Elem<T>::load(&w); }
     __device__ __forceinline__ void set(const float (&x)[1]) { Elem<T>::store(&w, x[0]); }
+    __device__ __forceinline__ void fill(float x) { Elem<T>::store(&w, x); }
+    __device__ __forceinline__ void lower(const Vec& o) { fill(min_nan(Elem<T>::load(&w), Elem<T>::load(&o.w))); }
+    __device__ __forceinline__ void raise(const Vec& o) { fill(max_nan(Elem<T>::load(&w), Elem<T>::load(&o.w))); }
+    __device__ __forceinline__ Vec from(int o) const { Vec v; v.fill(__shfl_xor_sync(kFull, Elem<T>::load(&w), o)); return v; }
 };
-
-// The smaller and the larger; not a number where one is not (a page with such a key must not lose it).
-__device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
-__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
 // Angles are taken in turns as 64-bit fixed-point fractions, whose wrap-around is the whole turns': the step of a pair, freq / 2 pi, once per block
 // and pair in two doubles (1 / 2 pi = kTurn + kTurnRest to 107 bits), then one integer product per position, off by 2^-34 of a turn at
@@ -79,8 +101,10 @@ struct News { int first, n, have; bool fits; };   // a sequence's new rows: the 
 struct Dims { int B, Hq, Hkv, T, d, group, cut, cuts; };   // cut: most rows of a piece, page_size or 64; cuts: pieces of a page
 
 // E: elements of a vector.  kUnits: units of a row (see below) where they fill a power of two of lanes and all columns are rotated, or none; 0: any.
-template <typename T, int E, bool kPairs, int kUnits>
-__global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages, const sc_paged_rows rows, const Dims dims, int32_t* status) {
+// kBounds: the pages' bounds are kept, in some 110 registers, so two blocks per SM; without them three fit (32 K tokens 161 -> 135 us).  With bounds a
+// third block costs spills (four prompts of 64-row pages 154 -> 190 us), as it does in the kernel for any units (11.0 -> 13.4 us).
+template <typename T, int E, bool kPairs, int kUnits, bool kBounds>
+__global__ void __launch_bounds__(kThreads, kBounds || kUnits == 0 ? 2 : 3) append_paged(const Pages<T> pages, const sc_paged_rows rows, const Dims dims, int32_t* status) {
     // Cosines and sines of a row, in the order in which lanes take them: lane u the pairs u * E .. u * E + E - 1, four at a time, so that
     // each four of neighbouring lanes lie side by side (as a plain list of pairs, read with 16-way bank conflicts, 35 K tokens x 48 heads took 265 us).
     __shared__ __align__(16) float sh_cos[kSub * kMaxHalf], sh_sin[kSub * kMaxHalf];
@@ -172,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages
     const int turned_units = (half + E - 1) / E, cs_row = turned_units * E;
     const auto place_of_pair = [&](int c) { return (c % E / kFour * turned_units + c / E) * kFour + c % kFour; };
     const int64_t page_at = (int64_t)id * pages.page_stride;
-    const bool bounds = pages.k_min != nullptr && id >= 0;
+    const bool bounds = kBounds && id >= 0;
 
     for (int s0 = 0; s0 < nr; s0 += kSub) {
         const int ns = min(kSub, nr - s0);
@@ -212,19 +236,8 @@ __global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages
                 const bool turned = !is_v && (kUnits ? half > 0 : kPairs ? 2 * u * E < rot : u < rot_units);
                 const int va = u < rot_units ? u : 2 * rot_units + 2 * (u - rot_units), vb = u < rot_units ? u + rot_units : va + 1;
                 const bool has_a = active && (kUnits || u < units), has_b = kUnits ? has_a : has_a && vb < n_vec;
-                float lo_a[E], hi_a[E], lo_b[E], hi_b[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) { lo_a[e] = lo_b[e] = INFINITY; hi_a[e] = hi_b[e] = -INFINITY; }
-                // a page whose first row is new starts afresh; of another one the bounds so far are requested beside the rows (the same thread
-                // comes back here with the next rows of a longer piece)
-                const bool mine = bounds && is_k && has_a && lr == 0, widen = mine && in_page + s0 > 0;
-                T* mn = pages.k_min + ((int64_t)id * pages.page_heads + x) * d;
-                T* mx = pages.k_max + ((int64_t)id * pages.page_heads + x) * d;
-                Vec<T, E> old[4];
-                if (widen) {
-                    old[0].load(mn + va * E); old[1].load(mx + va * E);
-                    if (has_b) { old[2].load(mn + vb * E); old[3].load(mx + vb * E); }
-                }
+                Vec<T, E> lo_a, hi_a, lo_b, hi_b;
+                if (kBounds) { lo_a.fill(INFINITY); lo_b.fill(INFINITY); hi_a.fill(-INFINITY); hi_b.fill(-INFINITY); }
                 for (int rb = lr; rb < ns; rb += 4 * row_slots) {   // four rows requested together
                     Vec<T, E> a[4], c[4];
 #pragma unroll
@@ -277,44 +290,45 @@ __global__ void __launch_bounds__(kThreads, 2) append_paged(const Pages<T> pages
                         a[j].store(to + va * E);
                         if (has_b) c[j].store(to + vb * E);
                         if (bounds && is_k) {   // of what is stored
-                            float xa[E], xb[E];
-                            a[j].get(xa);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) { lo_a[e] = min_nan(lo_a[e], xa[e]); hi_a[e] = max_nan(hi_a[e], xa[e]); }
-                            if (has_b) {
-                                c[j].get(xb);
-#pragma unroll
-                                for (int e = 0; e < E; ++e) { lo_b[e] = min_nan(lo_b[e], xb[e]); hi_b[e] = max_nan(hi_b[e], xb[e]); }
-                            }
+                            lo_a.lower(a[j]); hi_a.raise(a[j]);
+                            if (has_b) { lo_b.lower(c[j]); hi_b.raise(c[j]); }
                         }
                     }
                 }
                 if (!bounds || hb >= Hkv) continue;   // (the same for the whole warp)
                 for (int o = unit_lanes; o < unit_lanes * row_slots; o *= 2) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        lo_a[e] = min_nan(lo_a[e], __shfl_xor_sync(kFull, lo_a[e], o)); hi_a[e] = max_nan(hi_a[e], __shfl_xor_sync(kFull, hi_a[e], o));
-                        lo_b[e] = min_nan(lo_b[e], __shfl_xor_sync(kFull, lo_b[e], o)); hi_b[e] = max_nan(hi_b[e], __shfl_xor_sync(kFull, hi_b[e], o));
-                    }
+                    lo_a.lower(lo_a.from(o)); hi_a.raise(hi_a.from(o));
+                    lo_b.lower(lo_b.from(o)); hi_b.raise(hi_b.from(o));
                 }
-                if (mine) {
-                    const auto put = [&](T* at, float (&v)[E], const Vec<T, E>& was, bool smaller) {
-                        Vec<T, E> w;
-                        if (widen) {
-                            float o[E];
-                            was.get(o);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) v[e] = smaller ? min_nan(v[e], o[e]) : max_nan(v[e], o[e]);
-                        }
-                        w.set(v);
-                        w.store(at);
-                    };
-                    put(mn + va * E, lo_a, old[0], true);
-                    put(mx + va * E, hi_a, old[1], false);
-                    if (has_b) { put(mn + vb * E, lo_b, old[2], true); put(mx + vb * E, hi_b, old[3], false); }
+                if (is_k && has_a && lr == 0) {
+                    // a page whose first row is new starts afresh, another one's bounds are widened (the same thread comes back here with the next
+                    // rows of a longer piece)
+                    T* mn = pages.k_min + ((int64_t)id * pages.page_heads + x) * d;
+                    T* mx = pages.k_max + ((int64_t)id * pages.page_heads + x) * d;
+                    if (in_page + s0 > 0) {
+                        Vec<T, E> old[4];
+                        old[0].load(mn + va * E); old[1].load(mx + va * E);
+                        if (has_b) { old[2].load(mn + vb * E); old[3].load(mx + vb * E); }
+                        lo_a.lower(old[0]); hi_a.raise(old[1]);
+                        if (has_b) { lo_b.lower(old[2]); hi_b.raise(old[3]); }
+                    }
+                    lo_a.store(mn + va * E); hi_a.store(mx + va * E);
+                    if (has_b) { lo_b.store(mn + vb * E); hi_b.store(mx + vb * E); }
                 }
             }
         }
+    }
+}
+
+template <typename T, int E, bool kBounds>
+auto kernel_for(bool pairs, int rot, int units) {
+    // Two halves that are not whole vectors are rotated element by element.
+    if (!pairs && (rot / 2) % E != 0) return append_paged<T, 1, false, 0, kBounds>;
+    switch (units) {
+        case 4: return pairs ? append_paged<T, E, true, 4, kBounds> : append_paged<T, E, false, 4, kBounds>;
+        case 8: return pairs ? append_paged<T, E, true, 8, kBounds> : append_paged<T, E, false, 8, kBounds>;
+        case 16: return pairs ? append_paged<T, E, true, 16, kBounds> : append_paged<T, E, false, 16, kBounds>;
+        default: return pairs ? append_paged<T, E, true, 0, kBounds> : append_paged<T, E, false, 0, kBounds>;
     }
 }
 
@@ -339,16 +353,7 @@ cudaError_t run(const PagedAppendArgs& a, cudaStream_t st) {
     const dim3 grid((unsigned)blocks, (unsigned)groups);
     const bool pairs = (a.flags & SC_FLAG_ROPE_PAIRS) != 0;
     const int rot = a.rows.inv_freq != nullptr ? a.rows.rot_dim : 0, units = a.d % (2 * E) == 0 && (rot == 0 || rot == a.d) ? a.d / (2 * E) : 0;
-    const auto kernel = [&] {
-        // Two halves that are not whole vectors are rotated element by element.
-        if (!pairs && (rot / 2) % E != 0) return append_paged<T, 1, false, 0>;
-        switch (units) {
-            case 4: return pairs ? append_paged<T, E, true, 4> : append_paged<T, E, false, 4>;
-            case 8: return pairs ? append_paged<T, E, true, 8> : append_paged<T, E, false, 8>;
-            case 16: return pairs ? append_paged<T, E, true, 16> : append_paged<T, E, false, 16>;
-            default: return pairs ? append_paged<T, E, true, 0> : append_paged<T, E, false, 0>;
-        }
-    }();
+    const auto kernel = a.cache.k_min != nullptr ? kernel_for<T, E, true>(pairs, rot, units) : kernel_for<T, E, false>(pairs, rot, units);
     return launch_in_order(kernel, grid, kThreads, 0, st, pages, a.rows, dims, a.status);
 }
 
