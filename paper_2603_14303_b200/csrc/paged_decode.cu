@@ -321,6 +321,8 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
             l0 += __shfl_xor_sync(kFull, l0, off);
             l1 += __shfl_xor_sync(kFull, l1, off);
         }
+        if (l0 != l0) m0 = fmaxf(m0, 0.f);   // (no score was a number: not to be taken for a part without rows)
+        if (l1 != l1) m1 = fmaxf(m1, 0.f);
         if (g == 0) {
             sh_m[warp][2 * tig] = m0; sh_m[warp][2 * tig + 1] = m1;
             sh_l[warp][2 * tig] = l0; sh_l[warp][2 * tig + 1] = l1;

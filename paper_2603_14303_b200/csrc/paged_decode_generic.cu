@@ -214,6 +214,7 @@ paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq
 #pragma unroll
         for (int g = 0; g < kH; ++g) {
             const float lw = warp_sum(l[g]);
+            if (lw != lw) m[g] = fmaxf(m[g], 0.f);   // (no score was a number: not to be taken for a part without rows)
             if (lane == 0) { sh_m[warp][g] = m[g]; sh_l[warp][g] = lw; }
         }
         if (kH < kHeads && lane < kHeads - kH) { sh_m[warp][kH + lane] = -INFINITY; sh_l[warp][kH + lane] = 0.f; }

@@ -204,6 +204,24 @@ def test_values_that_are_not_finite_stay_in_their_head(flags):
     assert_close_vectors(torch.where(fine, got, 0.0).numpy(), torch.where(fine, want, 0.0).numpy(), TOL[BF], "attention")
 
 
+@pytest.mark.parametrize("dtype,flags", [(BF, 0), (BF, binding.SC_FLAG_GENERIC), (torch.float32, 0)])
+@pytest.mark.parametrize("lens", [(5, 100), (3000, 700), (40000, 9)])
+def test_scores_none_of_which_is_a_number(dtype, flags, lens):
+    """A query head of NaN, and keys of NaN in every row of a stretch: the outputs are not numbers, the other heads' are untouched."""
+    k, v, table, _ = _cache(dtype, 2, 2, 128, 16, [[n] for n in lens])
+    for page in table[1, 0, : -(-lens[1] // 16)].tolist():
+        k[page, 1, :, 3] = float("nan")
+    q = torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(3)).to(dtype)
+    q[0, 2, 17] = float("nan")
+    ln = torch.tensor([[n] for n in lens], dtype=torch.int32)
+    got = binding.paged_decode_attn(q.to(DEV), _device(k, v, table, None, "hnd"), ln.to(DEV), flags=flags).double().cpu()
+    assert bool(got[0, 2].isnan().all()) and bool(got[1, 4:].isnan().all())
+    want = pp.attention(q, k, v, table, ln)
+    fine = want.isfinite()
+    assert int(fine.sum()) == (7 + 4) * 128 and torch.equal(got.isfinite(), fine)
+    assert_close_vectors(torch.where(fine, got, 0.0).numpy(), torch.where(fine, want, 0.0).numpy(), TOL[dtype], "attention")
+
+
 def test_a_pool_past_32_bits():
     """Pages whose offsets pass 2^32 bytes and 2^31 elements."""
     P, ps, H, d = 140000, 16, 8, 128
