@@ -428,7 +428,8 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     // More units: single blocks, two per SM (128 units of 150 rows 12.8, in clusters of two 17.1); where units are long one per SM, which reads
     // fewer streams at a time (128 units of 6 K rows 71.8 and 73.9, of 12 K 124 and 128, of 16 K 166 and 175; but 512 of 1.5 K 73.0 and 69.7, 2048 of
     // 400 rows 111 and 78; 128 units of 3 K and 512 of 3 K the same).
-    // Tables of no more than 2.5 K rows, up to 16 units: clusters of eight, one per unit (8 units of 2 K rows 8.1 and 8.9, of 0.5 K 5.9 and 7.0).
+    // Tables of no more than 2.5 K rows, up to 16 units: clusters of eight, one per unit (8 units of 2 K rows 8.1, two clusters a unit 8.9, clusters of four
+    // 8.9; 16 units of 2.3 K rows 9.4, 12.3 with two; 8 of 0.5 K 5.9, of four 7.0).
     const bool small = units <= 16 && line.tiles_of(line.cap) <= 5 * 8 * kWarps;
     const int c = small ? 8 : units <= 64 ? 4 : 1;
     int blocks = sms * blocks_of(c, d);
@@ -438,7 +439,7 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     if (c > 1) {
         line.parties = blocks * 7 / 8 / c;
         int64_t most = (units * line.tiles_of(line.cap) + c * kWarps * kLeast - 1) / (c * kWarps * kLeast);   // what full tables could occupy
-        if (most < units) most = units;
+        if (most < units || small) most = units;
         if (most < line.parties) line.parties = (int)most;
         if (units <= line.parties && 8 * (line.parties % units) <= line.parties) line.parties -= (int)(line.parties % units);
         short_below = units <= 16 ? 0 : (unsigned)units * 512;
