@@ -346,8 +346,7 @@ struct Joiner {
         const unsigned first = me.cut ? me.party - me.own.index : p.at / me.stretch;
         const unsigned last = me.cut ? first + me.own.parts - 1 : (p.at + nt - 1) / me.stretch;
         int32_t* ticket = tickets + (first * me.csize + me.crank);   // (a party begins one shared unit at most)
-        __threadfence();
-        __syncthreads();
+        __syncthreads();   // (what the block's threads have written is released with the first one's arrival)
         if (threadIdx.x == 0) {
             int t;
             asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(t) : "l"(ticket) : "memory");
