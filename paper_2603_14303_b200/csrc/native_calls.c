@@ -217,6 +217,14 @@ static int list_of(PyObject* t, PyObject* type, long dev, int64_t n, void** at, 
     *at = address(t);
     return !PyErr_Occurred();
 }
+/* where the device's errors go: int32, at least one, or None */
+static int status_of(PyObject* t, long dev, void** at) {
+    *at = NULL;
+    if (t == Py_None) return 1;
+    if (!is_type(t, t_int32) || asked(t, s_get_device) != dev || asked(t, s_numel) < 1) return refuse("status", "int32 on the cache's device expected");
+    *at = address(t);
+    return !PyErr_Occurred();
+}
 /* after the cache: its type's object and number, its device, tables, heads and head dimension */
 typedef struct { PyObject* type; sc_dtype dt; long dev; int32_t B, heads, d; } about;
 static int about_of(PyObject* const* a, about* c) {
@@ -252,7 +260,8 @@ static PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     r.inv_freq = freq; r.rot_dim = 2 * (int32_t)freqs; r.positions = pos;
     const int32_t Hq = r.q != NULL ? (int32_t)q.heads : w.heads, T = (int32_t)k.n;
     const uint32_t flags = u32(a[25]);
-    void *status = address(a[24]), *stream = ptr(a[26]);
+    void *status, *stream = ptr(a[26]);
+    if (!status_of(a[24], w.dev, &status)) return NULL;
     CALL(sc_paged_append(&c, &r, w.dt, w.B, Hq, w.heads, T, w.d, flags, status, stream));
 }
 static int query_of(PyObject* t, const about* w, rows3* q, const char* what) {
@@ -271,12 +280,16 @@ static PyObject* paged_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_
     if (!query_of(t[0], &w, &q, "q") || !query_of(t[2], &w, &out, "out")) return NULL;
     if (q.heads != out.heads) { refuse("out", "the shape of q expected"); return NULL; }
     if (t[1] == Py_None || !list_of(t[1], t_int32, w.dev, (int64_t)w.B * c.table_heads, &lens, "lens")) { refuse("lens", "expected"); return NULL; }
-    if (asked(t[3], s_get_device) != w.dev) { refuse("workspace", "not on the cache's device"); return NULL; }
+    if (t[3] == Py_None || asked(t[3], s_get_device) != w.dev) { refuse("workspace", "expected on the cache's device"); return NULL; }
+    PyObject* whole = PyObject_CallMethodNoArgs(t[3], s_is_contiguous);
+    Py_XDECREF(whole);
+    if (whole != Py_True) { refuse("workspace", "not contiguous"); return NULL; }
     PyObject* bytes = PyObject_GetAttr(t[3], s_nbytes);
     if (!bytes) return NULL;
     const size_t have = sz(bytes);
     Py_DECREF(bytes);
-    void *ws = address(t[3]), *status = address(t[5]), *stream = ptr(t[7]);
+    void *ws = address(t[3]), *status, *stream = ptr(t[7]);
+    if (!status_of(t[5], w.dev, &status)) return NULL;
     const float scale = f32(t[4]);
     const uint32_t flags = u32(t[6]);
     CALL(sc_paged_decode_attn(&c, q.at, w.dt, w.B, (int32_t)q.heads, w.heads, w.d, lens, scale, flags, out.at, ws, have, status, stream));
@@ -295,7 +308,8 @@ static PyObject* paged_select(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     if (!list_of(t[1], t_int32, w.dev, (int64_t)w.B * c.table_heads, &lens, "lens") ||
         !list_of(t[5], t_int32, w.dev, (int64_t)w.B * w.heads * keep, &table, "sel_table") ||
         !list_of(t[6], t_int32, w.dev, (int64_t)w.B * w.heads, &len, "sel_len")) return NULL;
-    void *status = address(t[7]), *stream = ptr(t[8]);
+    void *status, *stream = ptr(t[8]);
+    if (!status_of(t[7], w.dev, &status)) return NULL;
     CALL(sc_paged_select(&c, q.at, w.dt, w.B, (int32_t)q.heads, w.heads, w.d, lens, keep, first, last, table, len, status, stream));
 }
 

@@ -120,6 +120,31 @@ def test_attention_and_selection_refused():
     assert binding.launch_counter() == before
 
 
+@pytest.mark.parametrize("status", [lambda: torch.zeros(1, dtype=torch.int32), lambda: _z(1, dtype=torch.int64), lambda: _z(0, **INT)],
+                         ids=["host", "long", "empty"])
+def test_status_words_refused(status):
+    c, q, lens = _cache(k_min=_z(6, 2, 16), k_max=_z(6, 2, 16)), _z(2, 2, 16), _i32(0, 0)
+    calls = [lambda s: binding.paged_append(c, _z(3, 2, 16), _z(3, 2, 16), _i32(0, 1, 3), _i32(0, 0), status=s),
+             lambda s: binding.paged_decode_attn(q, c, lens, status=s), lambda s: binding.paged_select(q, c, lens, 2, status=s)]
+    before = binding.launch_counter()
+    for call in calls:
+        with pytest.raises(ValueError, match="status"):
+            call(status())
+    assert binding.launch_counter() == before
+
+
+def test_workspaces_refused():
+    c, q, lens = _cache(), _z(2, 2, 16), _i32(0, 0)
+    size = binding.paged_decode_workspace(2, 2, 2, 16, DEV).numel()
+    before = binding.launch_counter()
+    for ws in (_z(1, dtype=torch.uint8).expand(size), torch.zeros(size, dtype=torch.uint8)):   # one byte shown many times; on the host
+        with pytest.raises(ValueError, match="workspace"):
+            binding.paged_decode_attn(q, c, lens, workspace=ws)
+    with pytest.raises(binding.ScError):
+        binding.paged_decode_attn(q, c, lens, workspace=_z(size - 16, dtype=torch.uint8))
+    assert binding.launch_counter() == before
+
+
 def test_one_launch_per_call():
     bounds = torch.zeros((6, 2, 16), dtype=BF, device=DEV)
     c = _cache(k_min=bounds, k_max=bounds.clone())
