@@ -63,9 +63,12 @@ struct Few { unsigned t[kCutEntries / 32]; };
 // Length of the line.  All lanes of a warp call it.
 __device__ __forceinline__ unsigned total_of(const Line& line, int lane, Few& few) {
     unsigned sum = 0;
+    int n[kCutEntries / 32];
+#pragma unroll
+    for (int i = 0; i < kCutEntries / 32; ++i) n[i] = line.lens[min(lane + 32 * i, line.entries - 1)];   // (unconditional: requested together)
 #pragma unroll
     for (int i = 0; i < kCutEntries / 32; ++i) {
-        few.t[i] = lane + 32 * i < line.entries ? line.tiles(lane + 32 * i) : 0;
+        few.t[i] = lane + 32 * i < line.entries ? line.tiles_of(max(min(n[i], line.cap), 0)) : 0;
         sum += few.t[i];
     }
 #pragma unroll 8
