@@ -71,8 +71,13 @@ __device__ __forceinline__ unsigned total_of(const Line& line, int lane, Few& fe
         few.t[i] = lane + 32 * i < line.entries ? line.tiles_of(max(min(n[i], line.cap), 0)) : 0;
         sum += few.t[i];
     }
-#pragma unroll 8
-    for (int e = kCutEntries + lane; e < line.entries; e += 32) sum += line.tiles(e);
+    for (int e0 = kCutEntries + lane; e0 < line.entries + lane; e0 += 8 * 32) {
+        int m[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = line.lens[min(e0 + 32 * i, line.entries - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += e0 + 32 * i < line.entries ? line.tiles_of(max(min(m[i], line.cap), 0)) : 0;
+    }
     return __reduce_add_sync(kFull, sum) * line.per_entry;
 }
 
