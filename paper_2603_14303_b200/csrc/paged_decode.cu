@@ -182,7 +182,8 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
         const Unit unit(pages, p.entry, p.unit, G, kHeads);
         s.nh = unit.nh;
         s.hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
-        const int each = (s.take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, s.take), t1 = p.tile + min((me.crank + 1) * each, s.take);
+        const int each = (s.take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, s.take);
+        const int t1 = min(p.tile + min((me.crank + 1) * each, s.take), Line::tiles_with_rows(len));
         s.first = t0 + warp;
         s.tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
         const int hp = pages.page_heads > 1 ? unit.h : 0;

@@ -70,7 +70,8 @@ paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq
         const int take = (int)min((unsigned)(nt - p.tile), me.left);
         const Unit unit(pages, p.entry, p.unit, G, kH);
         const int64_t hq0 = (int64_t)unit.b * Hq + unit.h * G + unit.g0;
-        const int each = (take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, take), t1 = p.tile + min((me.crank + 1) * each, take);
+        const int each = (take + me.csize - 1) / me.csize, t0 = p.tile + min(me.crank * each, take);
+        const int t1 = min(p.tile + min((me.crank + 1) * each, take), Line::tiles_with_rows(len));
         const int my_tiles = (t1 - t0 - warp + kWarps - 1) / kWarps;   // may be <= 0
         const int hp = pages.page_heads > 1 ? unit.h : 0;
         const T* kh = pages.k + hp * pages.head_stride;

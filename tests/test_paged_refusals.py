@@ -119,6 +119,8 @@ def test_more_rows_than_a_launch_can_number(lib):
     wide = dict(max_pages=2 ** 26, table_stride=2 ** 26)
     assert decode(lib, _cache(**wide), B=4, Hq=32, Hkv=8) == UNSUPPORTED      # 4 * 8 heads x 2^26 tiles of 16 rows
     assert decode(lib, _cache(**wide, page_heads=2), B=1, Hq=128, Hkv=2) == UNSUPPORTED   # 2 heads x 16 groups of queries
+    tiny = dict(page_heads=32, page_size=1, max_pages=1, table_stride=1)
+    assert decode(lib, _cache(**tiny), B=2 ** 25, Hq=32, Hkv=32) == UNSUPPORTED   # 2^30 heads, of four tiles at least
 
 
 def test_nothing_to_do(lib):
