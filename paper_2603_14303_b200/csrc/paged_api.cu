@@ -83,7 +83,7 @@ sc_status sc_paged_decode_attn(const sc_paged_cache* cache, const void* q, sc_dt
     if (s != SC_OK) return s;
     if (!(scale == scale) || scale < 0.f || (flags & ~SC_FLAG_GENERIC)) return SC_ERR_INVALID_ARG;
     const int64_t heads = (int64_t)B * Hkv * div_up(Hq / Hkv, 4);
-    if (heads * (((int64_t)cache->max_pages * cache->page_size + 63) / 64 * 4) > 0x7fffffff) return SC_ERR_UNSUPPORTED;   // 16-row tiles, in fours
+    if (heads * (((int64_t)cache->max_pages * cache->page_size + 63) / 64 * 4 + 4) > 0x7fffffff) return SC_ERR_UNSUPPORTED;   // 16-row tiles, in fours, and four more
     if (B == 0) return SC_OK;
     if (!q || !out || !lens || !workspace) return SC_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return SC_ERR_INVALID_ARG;

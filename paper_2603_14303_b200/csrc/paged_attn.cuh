@@ -46,11 +46,12 @@ constexpr size_t kTicketBytes = 4096;
 struct Line {
     const int32_t* lens;
     int entries, per_entry, cap, parties;   // per_entry: units of an entry
+    int spare;                              // tiles that every unit takes besides (see divide())
 
     __device__ __forceinline__ int len(int e) const { return max(min(lens[e], cap), 0); }
     // Of a unit of n rows: whole rounds of a block's warps, so that a unit of one row takes the place that its round does (512 sequences of 10 to
     // 100 rows 63 us, 86 without; 40 of 6 to 60 rows 8.2 and 21).  The tiles behind its rows are nobody's work.
-    __host__ __device__ __forceinline__ int tiles_of(int n) const { return n > 0 ? ((n - 1) / (kTile * kWarps) + 1) * kWarps : 0; }
+    __host__ __device__ __forceinline__ int tiles_of(int n) const { return n > 0 ? ((n - 1) / (kTile * kWarps) + 1) * kWarps + spare : 0; }
     __device__ __forceinline__ int tiles(int e) const { return tiles_of(len(e)); }
     static __host__ __device__ __forceinline__ int tiles_with_rows(int n) { return n > 0 ? (n - 1) / kTile + 1 : 0; }   // (n may be 2^31 - 1)
     // Positions on the line are 32-bit numbers, which the entry point sees to: several divisions lie on the way to the first load.

@@ -222,6 +222,17 @@ def test_scores_none_of_which_is_a_number(dtype, flags, lens):
     assert_close_vectors(torch.where(fine, got, 0.0).numpy(), torch.where(fine, want, 0.0).numpy(), TOL[dtype], "attention")
 
 
+@pytest.mark.parametrize("dtype,d,Hkv,G", [(BF, 128, 8, 4), (BF, 64, 4, 8), (F32, 64, 8, 2), (BF, 96, 8, 1)])
+@pytest.mark.parametrize("B", [40, 170])
+def test_many_short_sequences(dtype, d, Hkv, G, B):
+    """More heads than blocks, of no row, one, a round of a block's warps and one more."""
+    gen = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 150, (B,), generator=gen).tolist()
+    lens[:6] = [64, 65, 0, 1, 16, 63]
+    lens[-2:] = [129, 0]
+    _check(dtype, B, Hkv, G, d, 16, lens)
+
+
 def test_a_pool_past_32_bits():
     """Pages whose offsets pass 2^32 bytes and 2^31 elements."""
     P, ps, H, d = 140000, 16, 8, 128
