@@ -498,7 +498,7 @@ SC_API sc_status sc_paged_append(const sc_paged_cache* cache /*HOST*/, const sc_
  *              Calls that share a workspace must not overlap.
  *   status     SC_ERR_INVALID_ARG: a table named no page (its rows are left out of the sums); SC_ERR_TIMEOUT: a bounded
  *              wait inside the kernel gave up, the outputs it was for are not a number
- * A head without rows gets zeros.  B * Hkv * ceil(Hq / Hkv / 4) * (1 + ceil(max_pages * page_size / 64)) must stay below 2^29 (else
+ * A head without rows gets zeros, one with a score that is not a number NaN.  B * Hkv * ceil(Hq / Hkv / 4) * (1 + ceil(max_pages * page_size / 64)) must stay below 2^29 (else
  * SC_ERR_UNSUPPORTED).
  */
 SC_API size_t sc_paged_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
