@@ -451,7 +451,8 @@ typedef struct {
  *   rows (HOST)
  *     k, v        [T, Hkv, d], dtype dt, element strides kv_token, kv_head (16-byte multiples; d contiguous)
  *     count       [T, Hkv] int32, or NULL: written as 1 where the cache has counts (and refused where it has none)
- *     seq_off     [B + 1] int32 (device), not falling, 0 <= seq_off[b] <= T: sequence b's tokens start at seq_off[b]
+ *     seq_off     [B + 1] int32 (device), not falling, 0 <= seq_off[b] <= T: sequence b's tokens start at seq_off[b].  Where they fall,
+ *                 a sequence that starts before an offset in front of its own breaks the rules too (no token is two sequences')
  *     seq_len     [B] int32 (device) with 0 <= seq_len[b] <= seq_off[b+1] - seq_off[b], or NULL: all of that range.
  *                 Tokens outside every sequence's range are not looked at.
  *     cache_len   [B] int32 (device): rows each sequence holds already
@@ -469,7 +470,7 @@ typedef struct {
  *   flags       SC_FLAG_ROPE_PAIRS or 0
  *   status      SC_ERR_CAPACITY if a sequence's new rows do not all fit its table: its cache stays as it is and its
  *               len_out is cache_len (queries are rotated all the same).  SC_ERR_INVALID_ARG for offsets or lengths that
- *               break the rules above: that sequence is passed over.
+ *               break the rules above: that sequence is passed over, its len_out is cache_len.
  * No two sequences may append to the same page.  One kernel launch; no workspace.
  */
 typedef struct {

@@ -6,6 +6,10 @@
 // follow the most pieces there can be; which piece is a block's own it finds by counting all sequences' pieces.  (Places for two pieces more than
 // n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us.)
 // Sines and cosines of a piece's rows are taken once per block, 16 rows at a time, and shared by its heads.
+#include <limits.h>
+
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace sc {
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, kBounds || kUnits == 0 ? 2 : 3) appe
     __shared__ __align__(16) float sh_cos[kSub * kMaxHalf], sh_sin[kSub * kMaxHalf];
     __shared__ uint64_t sh_step[kMaxHalf];
     __shared__ News sh_news;
-    __shared__ int sh_seq, sh_piece, sh_sums[kWarps];
+    __shared__ int sh_seq, sh_piece, sh_sums[kWarps], sh_tops[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = pages.page_size, B = dims.B, Hkv = dims.Hkv, d = dims.d;
     if (tid == 0) sh_seq = -1;
@@ -118,8 +122,9 @@ __global__ void __launch_bounds__(kThreads, kBounds || kUnits == 0 ? 2 : 3) appe
     __syncthreads();
     const int rot = rows.inv_freq != nullptr ? rows.rot_dim : 0, half = rot / 2;
     for (int i = tid; i < half; i += kThreads) sh_step[i] = turn_step(rows.inv_freq[i]);
-    const auto news_of = [&](int b) {
+    const auto news_of = [&](int b, bool& falls) {
         const int o0 = rows.seq_off[b], o1 = rows.seq_off[b + 1], have = rows.cache_len[b];
+        falls = o1 < o0;
         const int n = rows.seq_len != nullptr ? rows.seq_len[b] : o1 - o0;
         const bool valid = o0 >= 0 && o1 >= o0 && o1 <= dims.T && n >= 0 && n <= o1 - o0 && have >= 0;
         return News{o0, valid ? n : -1, have, valid && (int64_t)have + n <= pages.cap()};
@@ -128,35 +133,62 @@ __global__ void __launch_bounds__(kThreads, kBounds || kUnits == 0 ? 2 : 3) appe
         if (!w.fits) set_status(status, w.n >= 0 ? SC_ERR_CAPACITY : SC_ERR_INVALID_ARG);
         if (rows.len_out != nullptr) rows.len_out[b] = w.fits ? w.have + w.n : w.have;
     };
-    if (blockIdx.y == 0 && B > kThreads)         // (fewer: in the loop below, by the first block)
-        for (int64_t b = (int64_t)blockIdx.x * kThreads + tid; b < B; b += (int64_t)gridDim.x * kThreads) tell((int)b, news_of((int)b));
     // pieces of `cut` rows of every page, numbered along a sequence's rows
     const unsigned cuts = dims.cuts;              // of a page
     const auto piece_of = [&](unsigned row) {     // (a length near 2^31 and rows that do not fit: below 2^32)
         const unsigned page = row / (unsigned)ps;
         return cuts == 1 ? page : page * cuts + (row - page * ps) / (unsigned)dims.cut;
     };
-    int before = 0;                              // pieces of the sequences so far
-    for (int b0 = 0; b0 < B && before <= (int)blockIdx.x; b0 += kThreads) {
-        const int b = b0 + tid;
-        int pieces = 0;
-        News w = {0, 0, 0, false};
-        if (b < B) {
-            w = news_of(b);
-            if (B <= kThreads && blockIdx.x == 0 && blockIdx.y == 0) tell(b, w);
-            if (w.n > 0) pieces = (int)(piece_of((unsigned)w.have + w.n - 1) - piece_of(w.have)) + 1;
-        }
-        const int upto = warp_scan_add(pieces, lane);
-        if (lane == 31) sh_sums[warp] = upto;
-        __syncthreads();
-        int first = before + upto - pieces;
+    // Sequences are counted in rounds of kThreads; those of the rounds x, x + gridDim.x, ... are told by block x.  Where offsets fall (then all rounds are
+    // gone through again, carefully) a sequence whose tokens start before an offset in front of its own is at fault too: ranges that lie apart have
+    // no more pieces than there are blocks, and no token is two sequences'.
+    const unsigned n_rounds = ((unsigned)B + kThreads - 1) / kThreads;
+    const auto count = [&](auto careful) {           // whether it has to be done carefully
+        unsigned tells = blockIdx.y == 0 ? blockIdx.x : n_rounds;
+        int before = 0, top = INT_MIN;               // pieces of the sequences so far; their largest offset
+        for (unsigned round = 0; round < n_rounds && (before <= (int)blockIdx.x || tells < n_rounds); ++round) {
+            const int b = (int)(round * kThreads + tid);
+            const bool is = (unsigned)b < (unsigned)B;   // (past 2^31 - 1 in the last round of the largest batches)
+            News w = {0, 0, 0, false};
+            bool falls = false;
+            if (is) w = news_of(b, falls);
+            if constexpr (careful) {
+                int most = warp_scan_max(is ? w.first : INT_MIN, lane);
+                if (lane == 31) sh_tops[warp] = most;
+                __syncthreads();
+                most = max(most, top);
+                for (int i = 0; i < kWarps; ++i) {
+                    if (i < warp) most = max(most, sh_tops[i]);
+                    top = max(top, sh_tops[i]);
+                }
+                if (is && w.first < most) { w.n = -1; w.fits = false; }
+            }
+            const int pieces = w.n > 0 ? (int)(piece_of((unsigned)w.have + w.n - 1) - piece_of(w.have)) + 1 : 0;
+            const int upto = warp_scan_add(pieces, lane);
+            const bool again = !careful && __any_sync(kFull, falls);
+            if (lane == 31) sh_sums[warp] = again ? -1 : upto;
+            __syncthreads();
+            int first = before + upto - pieces, signs = 0;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) {
-            first += i < warp ? sh_sums[i] : 0;
-            before += sh_sums[i];
+            for (int i = 0; i < kWarps; ++i) {
+                const int sum = sh_sums[i];
+                first += i < warp ? sum : 0;
+                before += sum;
+                signs |= sum;
+            }
+            if (!careful && signs < 0) return true;
+            if ((unsigned)((int)blockIdx.x - first) < (unsigned)pieces) { sh_seq = b; sh_piece = (int)blockIdx.x - first; sh_news = w; }
+            __syncthreads();
+            if (round == tells) {
+                if (is) tell(b, w);
+                tells += gridDim.x;
+            }
         }
-        if ((unsigned)((int)blockIdx.x - first) < (unsigned)pieces) { sh_seq = b; sh_piece = (int)blockIdx.x - first; sh_news = w; }
-        __syncthreads();
+        return false;
+    };
+    if (count(std::false_type())) {
+        __syncthreads();                             // (sh_sums is written again)
+        count(std::true_type());
     }
     const int b = sh_seq;
     if (b < 0) return;
