@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, kBounds || kUnits == 0 ? 2 : 3) appe
         falls = o1 < o0;
         const int n = rows.seq_len != nullptr ? rows.seq_len[b] : o1 - o0;
         const bool valid = o0 >= 0 && o1 >= o0 && o1 <= dims.T && n >= 0 && n <= o1 - o0 && have >= 0;
-        return News{o0, valid ? n : -1, have, valid && (int64_t)have + n <= pages.cap()};
+        return News{o0, valid ? n : -1, have, valid && (n == 0 || (int64_t)have + n <= pages.cap())};   // (no rows: they fit)
     };
     const auto tell = [&](int b, const News& w) {
         if (!w.fits) set_status(status, w.n >= 0 ? SC_ERR_CAPACITY : SC_ERR_INVALID_ARG);
