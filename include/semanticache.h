@@ -459,7 +459,9 @@ typedef struct {
  *     len_out     [B] int32 (device), may be NULL: cache_len[b] + its new rows.  Not cache_len itself: all layers of
  *                 a model append at the same place, so the lengths move on once per step, not once per call.
  *     q, q_out    [T, Hq, d] queries of the same tokens and where they go rotated; both NULL to skip.  Element strides
- *                 q_token, q_head and qo_token, qo_head (16-byte multiples); q_out may be q itself.
+ *                 q_token, q_head and qo_token, qo_head (16-byte multiples); q_out may be q itself.  The rows of what is
+ *                 written (q_out, and the cache's pools) must lie apart: in order of their strides, each axis of more than one entry
+ *                 steps over what the axes before it cover
  *     inv_freq    [rot_dim / 2] float (device), finite, of magnitude below 2^40, or NULL: no rotation;  rot_dim even, 0..d
  *     positions   [T] int32 (device), or NULL: a token's position is the row it gets
  *   cache       its tables are [B, 1, max_pages] and its pages hold all Hkv heads.  A cache with tables and pages per head is

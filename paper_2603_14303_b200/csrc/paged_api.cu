@@ -1,6 +1,8 @@
 // C-ABI entry points of the paged cache: argument validation and dispatch.  See include/semanticache.h.
 #include <math.h>
 
+#include <algorithm>
+
 #include "paged.cuh"
 
 using namespace sc;
@@ -39,6 +41,22 @@ sc_status check_pool(const sc_paged_cache* c, sc_dtype dt, int32_t d) {
     return SC_OK;
 }
 
+// Whether rows of d elements, one for every combination of the axes' indexes, lie apart: in order of their strides each axis of more than one entry
+// steps over what the axes before it cover, as the axes of any permuted view do, with gaps or without.
+struct Axis { int64_t n, stride; };
+bool apart(int64_t d, Axis a, Axis b, Axis c = {1, 0}) {
+    Axis axes[3] = {a, b, c};
+    if (a.n == 0 || b.n == 0 || c.n == 0) return true;
+    std::sort(axes, axes + 3, [](const Axis& x, const Axis& y) { return x.stride < y.stride; });
+    __int128 covered = d;
+    for (const Axis& x : axes) {
+        if (x.n == 1) continue;
+        if (x.stride < covered) return false;
+        covered += (__int128)(x.n - 1) * x.stride;
+    }
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -56,6 +74,8 @@ sc_status sc_paged_append(const sc_paged_cache* cache, const sc_paged_rows* rows
     if (rows->count != nullptr && cache->count == nullptr) return SC_ERR_INVALID_ARG;
     if ((cache->k_min == nullptr) != (cache->k_max == nullptr)) return SC_ERR_INVALID_ARG;
     if (!aligned16(cache->k_min) || !aligned16(cache->k_max)) return SC_ERR_INVALID_ARG;
+    if (!apart(d, {cache->num_pages, cache->page_stride}, {cache->page_heads, cache->head_stride}, {cache->page_size, cache->row_stride})) return SC_ERR_INVALID_ARG;
+    if (rows->q_out != nullptr && !apart(d, {T, rows->qo_token}, {Hq, rows->qo_head})) return SC_ERR_INVALID_ARG;
     if (B == 0) return SC_OK;
     if (rows->seq_off == nullptr || rows->cache_len == nullptr || rows->cache_len == rows->len_out) return SC_ERR_INVALID_ARG;
     if (T > 0 && (rows->k == nullptr || rows->v == nullptr)) return SC_ERR_INVALID_ARG;
