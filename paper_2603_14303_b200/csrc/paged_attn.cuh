@@ -188,7 +188,9 @@ struct Party {
         asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // (waited for before the first hand-over)
     }
     __device__ __forceinline__ void step() {      // every block of the cluster has started
-        if (!in_step) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        if (in_step) return;
+        __syncwarp();                             // (its callers come from branches and loops of some of a warp's threads)
+        asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
         in_step = true;
     }
     // Whether the block has anything to do.
@@ -407,6 +409,7 @@ struct Joiner {
     // their waits ends, and a thread that has left is not waited for) and what they handed over has landed.
     __device__ __forceinline__ void leave(const Party& me) {
         if (me.csize == 1 || __all_sync(kFull, got)) return;
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
         for (unsigned back = 1; back <= 2 && back <= turn; ++back) umma::mbar_wait<true>(smem_u32(&bar[(turn - back) & 1]), (turn - back) >> 1 & 1);
     }
