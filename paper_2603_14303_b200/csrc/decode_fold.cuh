@@ -30,12 +30,12 @@ __device__ __forceinline__ void hand_over(uint32_t dst, uint32_t bar, float x, f
                  ::"r"(dst), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)), "r"(bar) : "memory");
 }
 
-// Waits until everything the cluster's blocks hand this one has arrived.  The limit is by the clock, which runs on while a context is
-// switched off: a wait that ran out of it is given one more.
-__device__ __forceinline__ bool slices_arrived(uint32_t bar, unsigned long long limit_ns = umma::kWaitLimitNs) {
+// Waits until everything the cluster's blocks hand this one (in the barrier's phase of the given parity) has arrived.  The limit is by
+// the clock, which runs on while a context is switched off: a wait that ran out of it is given one more.
+__device__ __forceinline__ bool slices_arrived(uint32_t bar, unsigned long long limit_ns = umma::kWaitLimitNs, uint32_t parity = 0) {
     bool got = false;
 #pragma unroll 1
-    for (int turn = 0; turn < 2 && !got; ++turn) got = umma::mbar_wait<true>(bar, 0, limit_ns);
+    for (int turn = 0; turn < 2 && !got; ++turn) got = umma::mbar_wait<true>(bar, parity, limit_ns);
     return got;
 }
 

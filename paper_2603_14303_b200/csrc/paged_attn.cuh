@@ -310,6 +310,7 @@ struct Joiner {
     int heads;                   // most of a unit
     unsigned turn;               // of the segment: which barrier and place, and its phase
     bool got;                    // no wait has given up
+    unsigned long long limit_ns = umma::kWaitLimitNs;
 
     template <typename T, typename Sum, typename Ml>
     __device__ __forceinline__ void join(Party& me, const Place& p, int nt, int take, int nh, int d, T* __restrict__ out, Sum&& sum, Ml&& ml) {
@@ -348,7 +349,7 @@ struct Joiner {
                 const float2 v = ml(x & 7);
                 dm::hand_over(dm::mapa(smem_u32(recv_ml + me.crank * 2 * kHeads + (x & 7) * 2), x >> 3), dm::mapa(b, x >> 3), v.x, v.y);
             }
-            if (got) got = umma::mbar_wait<true>(b, turn >> 1 & 1);
+            if (got) got = dm::slices_arrived(b, limit_ns, turn >> 1 & 1);
             if (!got) set_status(status, SC_ERR_TIMEOUT);
             for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
                 const dm::Folded f = dm::fold_slices(recv_o, recv_ml, me.csize, slice, e4 - e_lo, e4 / d4n, got);
