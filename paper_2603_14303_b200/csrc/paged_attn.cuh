@@ -298,6 +298,11 @@ struct Finder {
 __host__ __device__ constexpr int recv_o_bytes(int d, int heads) { return (heads * (d / 4) + kCluster) * 16; }   // slices of O, rounded up
 __host__ __device__ constexpr int recv_bytes(int d, int heads) { return recv_o_bytes(d, heads) + kCluster * kHeads * 8; }   // and m, l
 
+// A block that gave up on a hand-over takes part in no other: for its later segments it hands nothing on and waits for nothing, and what it has to give
+// is not a number.  The cluster's other blocks miss its slices at the next segment and give up there.  So nobody's bytes come to a place or a phase that
+// is still in use: who hands something over for the segment after the next has had everybody's slices of the next one, and those a block hands on when it
+// is done with the one before.
+//
 // A segment's sums become results or go to whoever joins them.  sum(e4): four columns of a head (e4 = head * d / 4 + column / 4) over the
 // block's warps; ml(head): their m and l.  All threads of the block call it, behind a barrier; they may be anywhere in it when it returns.
 struct Joiner {
@@ -308,8 +313,8 @@ struct Joiner {
     float* part;
     int32_t* status;
     int heads;                   // most of a unit
-    unsigned turn;               // of the segment: which barrier and place, and its phase
-    bool got;                    // no wait has given up
+    unsigned turn;               // segments handed over: which barrier and place, and its phase
+    bool got;                    // no wait has given up: of this thread's in a segment, of the block's behind next()
     unsigned long long limit_ns = umma::kWaitLimitNs;
 
     template <typename T, typename Sum, typename Ml>
@@ -339,23 +344,28 @@ struct Joiner {
             unsigned char* to_me = recv + (turn & 1) * recv_bytes(d, heads);
             float4* recv_o = reinterpret_cast<float4*>(to_me);
             float* recv_ml = reinterpret_cast<float*>(to_me + recv_o_bytes(d, heads));
-            if (threadIdx.x == 0) umma::mbar_expect_tx(b, (uint32_t)(me.csize * ((e_hi - e_lo) * 16 + kHeads * 8)));
-            me.step();
-            for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
-                const int to = e4 / slice;
-                dm::hand_over(dm::mapa(smem_u32(recv_o + me.crank * slice + (e4 - to * slice)), to), dm::mapa(b, to), sum(e4));
+            if (got) {
+                if (threadIdx.x == 0) umma::mbar_expect_tx(b, (uint32_t)(me.csize * ((e_hi - e_lo) * 16 + kHeads * 8)));
+                me.step();
+                for (int e4 = threadIdx.x; e4 < n4; e4 += kThreads) {
+                    const int to = e4 / slice;
+                    dm::hand_over(dm::mapa(smem_u32(recv_o + me.crank * slice + (e4 - to * slice)), to), dm::mapa(b, to), sum(e4));
+                }
+                for (int x = threadIdx.x; x < me.csize * kHeads; x += kThreads) {
+                    const float2 v = ml(x & 7);
+                    dm::hand_over(dm::mapa(smem_u32(recv_ml + me.crank * 2 * kHeads + (x & 7) * 2), x >> 3), dm::mapa(b, x >> 3), v.x, v.y);
+                }
+                got = dm::slices_arrived(b, limit_ns, turn >> 1 & 1);
+                if (!got) set_status(status, SC_ERR_TIMEOUT);
+                ++turn;
             }
-            for (int x = threadIdx.x; x < me.csize * kHeads; x += kThreads) {
-                const float2 v = ml(x & 7);
-                dm::hand_over(dm::mapa(smem_u32(recv_ml + me.crank * 2 * kHeads + (x & 7) * 2), x >> 3), dm::mapa(b, x >> 3), v.x, v.y);
-            }
-            if (got) got = dm::slices_arrived(b, limit_ns, turn >> 1 & 1);
-            if (!got) set_status(status, SC_ERR_TIMEOUT);
             for (int e4 = e_lo + threadIdx.x; e4 < e_hi; e4 += kThreads) {
-                const dm::Folded f = dm::fold_slices(recv_o, recv_ml, me.csize, slice, e4 - e_lo, e4 / d4n, got);
+                dm::Folded f = dm::fold_slices(recv_o, recv_ml, me.csize, slice, e4 - e_lo, e4 / d4n, got);
+                // Where they have not all arrived, m and l as well: they come from every slice of a head, the last one to be stored stays, and
+                // whichever m and l are left together give these columns as NaN and the head's others right or as NaN.
+                if (!got) { f.m = INFINITY; f.l = __int_as_float(0x7fffffff); }
                 give(e4, f.o, f.m, f.l);
             }
-            ++turn;
         }
         if (whole) return;
         // Parties that share a unit: the last one to bring a slice joins the slice's parts in order.
@@ -406,13 +416,18 @@ struct Joiner {
             store_out4(out + (int64_t)hd * d + d4, acc, l);
         }
     }
+    // Between two segments, in place of a barrier of the block's threads.
+    __device__ __forceinline__ void next(const Party& me) {
+        if (me.csize == 1) __syncthreads(); else got = __syncthreads_and(got);
+    }
     // The last step.  Where a hand-over was given up on, the block's shared memory stays until the cluster's other blocks have left (each of
-    // their waits ends, and a thread that has left is not waited for) and what they handed over has landed.
+    // their waits ends, and a thread that has left is not waited for) and what they handed over has landed: of the last phase that was
+    // waited for here; who handed something over for the one after it has waited for this block's slices meanwhile, to the limit.
     __device__ __forceinline__ void leave(const Party& me) {
         if (me.csize == 1 || __all_sync(kFull, got)) return;
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-        for (unsigned back = 1; back <= 2 && back <= turn; ++back) umma::mbar_wait<true>(smem_u32(&bar[(turn - back) & 1]), (turn - back) >> 1 & 1);
+        umma::mbar_wait<true>(smem_u32(&bar[(turn - 1) & 1]), (turn - 1) >> 1 & 1, limit_ns);
     }
 };
 

@@ -369,7 +369,7 @@ paged_decode_mma(const Pages<const bf16> pages, const bf16* __restrict__ q, int 
         joiner.join(me, seg.p, seg.nt, seg.take, nh, D, out + hq0 * D, block_sum, block_ml);
         if (last) break;
         me.left -= seg.take;
-        __syncthreads();   // the sums' place, sh_m and sh_l are written again, and the ring where it is that place
+        joiner.next(me);   // the sums' place, sh_m and sh_l are written again, and the ring where it is that place
         if (apart) {
             seg = then;
         } else {

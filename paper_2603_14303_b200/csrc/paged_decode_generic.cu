@@ -259,7 +259,7 @@ paged_decode_generic(const Pages<const T> pages, const T* __restrict__ q, int Hq
         me.left -= take;
         if (me.left == 0) break;
         next_unit(line, p, nt);
-        __syncthreads();   // the ring, sq, sh_m and sh_l are written again
+        joiner.next(me);   // the ring, sq, sh_m and sh_l are written again
     }
     zero_empty(pages, line, Hq, G, kH, d, out);
     joiner.leave(me);

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) probe(Line line, const Division how,
             me.left -= take;
             if (me.left == 0) break;
             next_unit(line, p, nt);
-            __syncthreads();
+            joiner.next(me);
         }
         joiner.leave(me);
     } else {

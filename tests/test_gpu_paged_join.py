@@ -86,3 +86,58 @@ def test_a_block_later_than_one_limit(probe, rows, parties, cluster, segment):
     out, status, _ = probe(rows, parties, cluster, late=1, segment=segment, delay_ms=75, limit_ms=50)
     assert status == binding.SC_OK
     np.testing.assert_allclose(out, expected(rows, parties, cluster), rtol=1e-5)
+
+
+def _late_by_too_much(probe, rows, parties, cluster, segment, late):
+    """`late` (of the first cluster) is later than both limits.  What is a number is right, the rest is what it has to be."""
+    want, seg = expected(rows, parties, cluster), segments(rows, parties, cluster)
+    out, status, left = probe(rows, parties, cluster, late=late, segment=segment, delay_ms=150, limit_ms=30)
+    assert status == binding.SC_ERR_TIMEOUT
+    fine = np.isfinite(out)
+    np.testing.assert_allclose(out[fine], want[fine], rtol=1e-5)
+    mine = seg[0]
+    for p in range(1, parties):                                     # the other clusters' own units
+        for u in seg[p]:
+            assert u in mine or fine[u].all()
+    for u in mine[:segment]:                                        # before it was late
+        assert fine[u].all()
+    n4 = HEADS * D // 4
+    size = -(-n4 // cluster)
+    own = np.zeros(n4, bool)
+    own[late * size:(late + 1) * size] = True                       # the late block's slice, for which it had everybody's sums
+    own = np.repeat(own, 4).reshape(HEADS, D)
+    for i, u in enumerate(mine[segment:]):
+        shared = any(u in seg[p] for p in range(1, parties))
+        if i > 0:
+            assert not fine[u].any()
+        else:
+            assert not fine[u][~own].any() and (shared or fine[u][own].all())
+    if segment == len(mine) - 1:                                    # those that gave up leave after the one that did not
+        assert (left[:cluster] >= left[late] - 5 * MS).all()
+    return out
+
+
+@pytest.mark.parametrize("rows,parties,cluster", LINES)
+@pytest.mark.parametrize("segment", [0, 1, 2, -1])
+def test_a_block_later_than_both_limits(probe, rows, parties, cluster, segment):
+    """From the segment on that it was late for nothing is handed on: no sum is made of two segments' slices."""
+    _late_by_too_much(probe, rows, parties, cluster, segment % len(segments(rows, parties, cluster)[0]), late=1)
+
+
+def test_any_block_may_be_late(probe):
+    rows, parties, cluster = LINES[3]
+    for late in range(cluster):
+        _late_by_too_much(probe, rows, parties, cluster, 3, late)
+        out, status, _ = probe(rows, parties, cluster)              # and the next launch is as if nothing had been
+        assert status == binding.SC_OK
+        np.testing.assert_allclose(out, expected(rows, parties, cluster), rtol=1e-5)
+
+
+def test_a_shared_unit_one_of_whose_parts_is_not_complete(probe):
+    """The unit that two clusters share, with the first one late for it: whoever joins the parts, they give NaN."""
+    rows, parties, cluster = LINES[2]
+    seg = segments(rows, parties, cluster)
+    shared = seg[0][-1]
+    assert shared in seg[1]
+    out = _late_by_too_much(probe, rows, parties, cluster, len(seg[0]) - 2, late=2)   # late for the one before: nothing of the shared one is handed on
+    assert np.isnan(out[shared]).all()
