@@ -445,8 +445,8 @@ typedef struct {
  *
  * The rotation (inv_freq not NULL) turns each pair (x1, x2) of the first rot_dim columns of a key or query by the angle
  * a_i = position * inv_freq[i]:  y1 = x1 cos a_i - x2 sin a_i,  y2 = x2 cos a_i + x1 sin a_i.  The angle is taken in 64-bit
- * fractions of a turn, so far positions lose nothing; products in fp32, one rounding to dt.  Values and the columns behind
- * rot_dim are copied.
+ * fractions of a turn, so far positions lose nothing; what is left of it, within half a turn, is rounded to 24 bits for sine and cosine
+ * (at most 9.4e-8); products in fp32, one rounding to dt.  Values and the columns behind rot_dim are copied.
  *
  *   rows (HOST)
  *     k, v        [T, Hkv, d], dtype dt, element strides kv_token, kv_head (16-byte multiples; d contiguous)
@@ -454,7 +454,7 @@ typedef struct {
  *     seq_off     [B + 1] int32 (device), not falling, 0 <= seq_off[b] <= T: sequence b's tokens start at seq_off[b].  Where they fall,
  *                 a sequence that starts before an offset in front of its own breaks the rules too (no token is two sequences')
  *     seq_len     [B] int32 (device) with 0 <= seq_len[b] <= seq_off[b+1] - seq_off[b], or NULL: all of that range.
- *                 Tokens outside every sequence's range are not looked at.
+ *                 Tokens outside every sequence's range are not looked at, their rows of q_out stay as they were.
  *     cache_len   [B] int32 (device): rows each sequence holds already
  *     len_out     [B] int32 (device), may be NULL: cache_len[b] + its new rows.  Not cache_len itself: all layers of
  *                 a model append at the same place, so the lengths move on once per step, not once per call.
@@ -490,7 +490,9 @@ SC_API sc_status sc_paged_append(const sc_paged_cache* cache /*HOST*/, const sc_
  * One decode step of Proportional Attention over a paged cache: sc_decode_attn with the rows found through the tables.
  *     x_t = scale * <q, k_t> + ln(count_t),  out = sum_t softmax(x)_t * v_t   over the rows t < lens[b, ht]
  * The rows of all sequences are shared out evenly among the launch's blocks whatever the lengths are; a head that
- * several blocks (or clusters of blocks) share is joined at the end in a fixed order.
+ * several blocks (or clusters of blocks) share is joined at the end in a fixed order.  Scores, maxima and sums are held in fp32.  The
+ * bf16 kernels for d = 64, 128 and 256 multiply the values by weights rounded to 16 bits (two bf16 each) and divide by the sum of the same rounded weights,
+ * which is off by some 2e-6 before the output's own rounding; the generic kernels keep weights in fp32.
  *
  *   q, out     [B, Hq, d] contiguous, dtype dt
  *   lens       [B, table_heads] int32 (device); more than max_pages * page_size counts as that many, below 0 as none
@@ -500,9 +502,10 @@ SC_API sc_status sc_paged_append(const sc_paged_cache* cache /*HOST*/, const sc_
  *              arrival counters must be zero on entry and are left zero: zero the workspace once after allocating it.
  *              Calls that share a workspace must not overlap.
  *   status     SC_ERR_INVALID_ARG: a table named no page (its rows are left out of the sums); SC_ERR_TIMEOUT: a bounded
- *              wait inside the kernel gave up, the outputs it was for are not a number
- * A head without rows gets zeros, one with a score that is not a number NaN.  B * Hkv * ceil(Hq / Hkv / 4) * (1 + ceil(max_pages * page_size / 64)) must stay below 2^29 (else
- * SC_ERR_UNSUPPORTED).
+ *              wait inside the kernel gave up, the outputs it was for are not a number, nor those of the heads that the same blocks had
+ *              still to do
+ * A head without rows, or all of whose scores are minus infinity, gets zeros, one with a score that is not a number NaN.
+ * B * Hkv * ceil(Hq / Hkv / 4) * (1 + ceil(max_pages * page_size / 64)) must stay below 2^29 (else SC_ERR_UNSUPPORTED).
  */
 SC_API size_t sc_paged_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
 
@@ -515,7 +518,8 @@ SC_API sc_status sc_paged_decode_attn(const sc_paged_cache* cache /*HOST*/, cons
  *     bound_p = max over the head's queries g of  sum_c max(q_gc * k_min[p, h, c], q_gc * k_max[p, h, c])
  * which no <q_g, k_t> of the page's rows exceeds.  The first n_first and the last n_last pages of a sequence are always
  * among them.  Equal bounds: the earlier page.  A bound that is not a number ranks above all numbers.  The choice is the one that
- * bounds in 64 bits give.
+ * bounds in 64 bits give.  Counts have no part in it: over a cache of cores, whose scores are scale * <q, k_t> + ln(count_t), a page is ranked as if
+ * all its counts were 1, and pages whose cores stand for many tokens come too low by as much as ln(count).
  * The result is a table for sc_paged_decode_attn (the same cache with table = sel_table, table_heads = Hkv, max_pages =
  * table_stride = keep, and lens = sel_len): attention over the pages picked costs what keep pages cost, however long the cache.
  *
@@ -525,7 +529,8 @@ SC_API sc_status sc_paged_decode_attn(const sc_paged_cache* cache /*HOST*/, cons
  *   sel_table   out [B, Hkv, keep] int32: the picked pages' table entries in the order of their rows; -1 behind them where a
  *               sequence has fewer pages (all of them are picked then)
  *   sel_len     out [B, Hkv] int32: rows in the picked pages
- *   status      SC_ERR_INVALID_ARG: a table named no page; its bound ranks below all others
+ *   status      SC_ERR_INVALID_ARG: a table named no page among those that are compared; its bound ranks below all others.  (Entries that are
+ *               picked without a comparison are handed on as they are: the always picked ones, and all where there are no more than keep.)
  * max_pages at most SC_SELECT_MAX_PAGES (else SC_ERR_UNSUPPORTED).  One kernel launch; no workspace.
  */
 #define SC_SELECT_MAX_PAGES 131072

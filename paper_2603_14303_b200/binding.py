@@ -674,7 +674,8 @@ def sc_paged_select(q, cache: PagedCache, lens, keep, n_first, n_last, sel_table
 def paged_append(cache: PagedCache, k_new, v_new, seq_off, cache_len, *, seq_len=None, count_new=None, inv_freq=None, positions=None,
                  interleaved: bool = False, q=None, q_out=None, len_out=None, status=None):
     """New rows join a paged cache, keys (and queries) rotated on the way.  Returns (the sequences' new lengths, the rotated
-    queries or None).  All layers of a model append at the same ``cache_len``: move it on once per step."""
+    queries or None).  All layers of a model append at the same ``cache_len``: move it on once per step.  Rows of the queries whose tokens
+    belong to no sequence are not written: where they matter (a padded batch), give ``q_out``."""
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if len_out is None:
@@ -704,7 +705,8 @@ def paged_decode_workspace(B, Hq, Hkv, d, device) -> torch.Tensor:
 
 
 def paged_decode_attn(q, cache: PagedCache, lens, out=None, workspace=None, scale: float = 0.0, status=None, flags: int = 0):
-    """One decode step of Proportional Attention over a paged cache (plain attention where it has no counts)."""
+    """One decode step of Proportional Attention over a paged cache (plain attention where it has no counts).  Without a ``workspace`` every
+    call allocates and zeroes one (7.4 MB)."""
     if out is None:
         out = torch.empty_like(q)
     if workspace is None:
@@ -716,7 +718,8 @@ def paged_decode_attn(q, cache: PagedCache, lens, out=None, workspace=None, scal
 
 def paged_select(q, cache: PagedCache, lens, keep: int, n_first: int = 0, n_last: int = 1, status=None):
     """Picks pages for sparse attention.  Returns (table [B, Hkv, keep], lengths [B, Hkv]) for
-    ``paged_decode_attn(q, cache.over(table), lengths)``."""
+    ``paged_decode_attn(q, cache.over(table), lengths)``.  Pages are ranked by their keys alone: over a cache of cores the counts, which add
+    ln(count) to the scores, have no part in it."""
     table = torch.empty((cache.B, cache.Hkv, keep), dtype=torch.int32, device=q.device)
     lengths = torch.empty((cache.B, cache.Hkv), dtype=torch.int32, device=q.device)
     sc_paged_select(q, cache, lens, keep, n_first, n_last, table, lengths, status)

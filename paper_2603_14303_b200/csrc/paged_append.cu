@@ -4,7 +4,8 @@
 // heads (keys, values and queries counted in one row).  So a page's bounds belong to one block per head, whose warps hold whole heads: smallest and
 // largest key are taken in registers over the piece's rows, as stored and two at a time in bf16, and meet in a few shuffles; no atomics.  The host knows T and B only, from which
 // follow the most pieces there can be; which piece is a block's own it finds by counting all sequences' pieces.  (Places for two pieces more than
-// n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us.)
+// n / page_size per sequence, found without counting, were half empty where every sequence has one token: 256 of them 9.3 us, counted 5.9.  Every block
+// counts the sequences before its own, 256 at a time: 2000 single tokens 51 us, 4096 (four heads) 80.)
 // Sines and cosines of a piece's rows are taken once per block, 16 rows at a time, and shared by its heads.
 #include <limits.h>
 
@@ -86,8 +87,9 @@ template <typename T> struct Vec<T, 1> {
 };
 
 // Angles are taken in turns as 64-bit fixed-point fractions, whose wrap-around is the whole turns': the step of a pair, freq / 2 pi, once per block
-// and pair in two doubles (1 / 2 pi = kTurn + kTurnRest to 107 bits), then one integer product per position, off by 2^-34 of a turn at
-// the farthest position.  (In doubles per position and pair it was a quarter of all instructions of a long prompt.)
+// and pair in two doubles (1 / 2 pi = kTurn + kTurnRest to 107 bits), off by 2^-62.6 of a turn, then one integer product per position, off by 2^-31.6
+// of a turn at the farthest position (2^31), 2^-45 at 128 K.  It is cut to 2^-32 of a turn and rounded to 24 bits, at most 2^-26 of a turn, for
+// sincospif.  (In doubles per position and pair it was a quarter of all instructions of a long prompt.)
 constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;
 __device__ __forceinline__ uint64_t turn_step(float freq) {
     const double f = freq, hi = f * kTurn, lo = fma(f, kTurn, -hi) + f * kTurnRest;

@@ -8,6 +8,9 @@
 //     P^T = 2^(x - m)          (online softmax in fp32; the running maximum is common to the warp and raised only when a score
 //                               overtakes it by a margin, so weights stay below 2^8)
 //     O^T[d x 8 heads] += V_tile^T . P^T                     (P as a bf16 pair, leading part + remainder: sixteen bits of each weight)
+// The sum of weights is taken over the same sixteen bits, so a weight's rounding moves the output towards or away from its own row only: some 2e-6
+// of it, a thousandth of the rounding to bf16 that follows (an output that close to the middle between two bf16 values may go to the other).  A third bf16 of each weight
+// would take a product more.
 // Up to four query heads stand in the eight columns twice, the second time for the remainders.  Warps meet in shared memory, blocks of a
 // cluster hand each other slices of their sums through distributed shared memory (decode_fold.cuh), parties that share a unit leave
 // partial sums in global memory, slice by slice, and the last to arrive joins them.  Every order is fixed: results are bit-reproducible.
@@ -430,7 +433,8 @@ Division divide(Line& line, int sms, int (*blocks_of)(int cluster, int d), int d
     // fewer streams at a time (128 units of 6 K rows 71.8 and 73.9, of 12 K 124 and 128, of 16 K 166 and 175; but 512 of 1.5 K 73.0 and 69.7, 2048 of
     // 400 rows 111 and 78; 128 units of 3 K and 512 of 3 K the same).
     // Tables of no more than 2.5 K rows, up to 16 units: clusters of eight, one per unit (8 units of 2 K rows 8.1, two clusters a unit 8.9, clusters of four
-    // 8.9; 16 units of 2.3 K rows 9.4, 12.3 with two; 8 of 0.5 K 5.9, of four 7.0).
+    // 8.9; 16 units of 2.3 K rows 9.4, 12.3 with two; 8 of 0.5 K 5.9, of four 7.0).  This goes by the tables' width, since lengths are known on the device
+    // only: the same rows in tables for 128 K rows take clusters of four (8 units of 2 K 9.1, 16 of 2.3 K 9.9, 8 of 0.5 K 7.0).
     line.spare = 0;
     const bool small = units <= 16 && line.tiles_of(line.cap) <= 5 * 8 * kWarps;
     const int c = small ? 8 : units <= 64 ? 4 : 1;
